@@ -243,6 +243,96 @@ ic_status ic_distill_loss(const float *const *probs, int32_t n_targets, const fl
                           double *loss_multi, double *loss_avg, float *grad, void *workspace, size_t workspace_bytes,
                           void *stream);
 
+/*
+ * A key-value cache in 4 bits, with the attention that reads it.
+ *
+ * A row of IC_KV4_ROW_BYTES bytes holds one 576-element latent KV row (512 latent features, then 64 rotary ones):
+ *   bytes   0..255  feature f < 512 as a 4-bit float (sign, two exponent bits, one fraction bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6)
+ *                   in the low (f even) or high (f odd) half of byte f / 2
+ *   bytes 256..383  features 512..575, bf16
+ *   bytes 384..387  one byte 127 + e_j per 128 latent features: their values are code * 2^e_j
+ *   bytes 388..399  zero
+ * e_j is the least e in [-100, 100] with max |x| <= 6 * 2^e over the block; codes are the nearest, ties to the even code,
+ * larger values (only where e_j = 100) become 6 * 2^100.  A block that holds an infinity or a NaN has the byte 255 and reads
+ * as NaN throughout.  Every value that a row can hold is a bf16.
+ *
+ * KV4 is [B, Lk, 400 bytes] or, with a page table, a pool of pool_rows rows; its address is a multiple of 16.  pool_rows is
+ * the number of rows that KV4 holds in either case (B * Lk at least in the dense one, below 2^31): a row number outside it,
+ * from whatever a page table holds, is neither read nor written.  pc: NULL, or lengths and / or a page table as above.
+ *
+ * ic_kv4_write: rows [B, Tn, 576] bf16 into the cache: row i of sequence b goes to position pos0 + i, or with seq_lens to
+ *   position seq_lens[b] - Tn + i (the last Tn positions; pos0 is ignored).  Positions outside [0, min(Lk, seq_lens[b])) are
+ *   left out, and nothing else of the cache changes.
+ * ic_kv4_read: the same positions back as bf16 rows [B, Tn, 576]; zeros for positions that are left out.
+ *
+ * ic_sparse_attn_kv4: ic_sparse_attn over such a cache: the same as over the rows that ic_kv4_read returns, with
+ *   desc->d_qk = row_elems = 576, d_v = 512, v_off = 0.  With seq_lens, entries of idx at or behind seq_lens[b] are skipped too.
+ *   A skipped entry's row never matters, whatever it holds.
+ * ic_attn_probs_kv4: ic_attn_probs over such a cache; lse as ic_sparse_attn_kv4 returns it.  Rows without a valid entry give
+ *   zeros (their lse is not used).
+ * Q, rows and O: addresses that are multiples of 16.  Asynchronous; errors as elsewhere, IC_ERR_SHAPE for a bad address.
+ */
+#define IC_KV4_ROW_BYTES 400
+typedef struct ic_kv4_desc {
+    int32_t B;         /* sequences */
+    int32_t Tn;        /* rows per sequence of this call */
+    int32_t Lk;        /* positions per sequence, or the bound on them */
+    int32_t reserved;  /* 0 */
+    int64_t pos0;      /* position of row 0 where pc gives no seq_lens */
+    int64_t pool_rows; /* rows that KV4 holds */
+} ic_kv4_desc;
+ic_status ic_kv4_write(const ic_kv4_desc *d, const ic_paged_cache *pc, const void *rows, void *KV4, void *stream);
+ic_status ic_kv4_read(const ic_kv4_desc *d, const ic_paged_cache *pc, const void *KV4, void *rows, void *stream);
+size_t ic_sparse_attn_kv4_workspace(const ic_attn_desc *desc);
+ic_status ic_sparse_attn_kv4(const ic_attn_desc *desc, const ic_paged_cache *pc, int64_t pool_rows, const void *Q, const void *KV4,
+                             const int32_t *idx, void *O, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+ic_status ic_attn_probs_kv4(const ic_attn_desc *desc, const ic_paged_cache *pc, int64_t pool_rows, const void *Q, const void *KV4,
+                            const int32_t *idx, const float *lse, float *probs, void *stream);
+
+/*
+ * Eviction from a cache by accumulated attention weight.
+ *
+ * ic_attn_weight_add: what each position received,
+ *     weight[b,s] = weight_in[b,s] + sum over t, m with idx[b,t,m] = s of probs[b,t,m]
+ *   probs, idx [B,Tq,k_sel] as ic_attn_probs and ic_indexer_topk leave them (entries outside [0, Lk) are skipped, equal
+ *   entries of a row all count); weight_in [B,Lk] fp32, nullable (zeros), may be weight itself; weight [B,Lk] fp32 out.
+ *   A probability below 0 or not a number counts as 0, one above 1 as 1; each is taken to 2^-48, and their sum is the same
+ *   whatever the order.  workspace: ic_attn_weight_add_workspace() bytes (0 for a few rows).
+ *
+ * ic_evict_keep: the positions of each sequence that stay when at most n_keep do.  A sequence of n = min(Lk, seq_lens[b])
+ *   positions (seq_lens NULL: Lk) keeps all if n <= n_keep; otherwise the first n_first, the last n_recent, and of the
+ *   others those with the largest weight[b,s] up to n_keep in all (equal weights: the lower position; NaN counts as the
+ *   largest).  n_first + n_recent <= n_keep <= Lk.
+ *   keep [B,n_keep] int32 out: the positions in ASCENDING order, then -1;  keep_lens [B] int32 out: their number, the new
+ *   seq_lens;  keep_weight [B,n_keep] fp32 out, nullable: weight at those positions (0 behind them), the new weight.
+ *   workspace: ic_evict_keep_workspace(B, Lk) bytes.
+ *
+ * ic_cache_compact: rows of n_caches caches (host array, at most IC_MAX_MOVE_CACHES; each with rows of its own width, a
+ *   multiple of 4 bytes) to their new positions: row keep[b][j] of sequence b becomes row j.  src: [B,Lk,row_bytes], or the
+ *   pool of src_pc's page table; dst: [B,n_keep,row_bytes], or the pool of dst_pc's (which covers n_keep positions).  The
+ *   seq_lens of both are ignored.  Rows behind a sequence's last kept one stay as they were, as does the rest of a pool.  The
+ *   rows written must be none of the rows read: src and dst ranges may not meet, except as one pool with different page
+ *   tables whose pages differ.  src_rows, dst_rows: rows that the buffers hold; row numbers outside them are left out.
+ */
+#define IC_MAX_MOVE_CACHES 16
+typedef struct ic_cache_move {
+    const void *src;
+    void *dst;
+    int64_t src_rows;
+    int64_t dst_rows;
+    int32_t row_bytes;
+    int32_t reserved;  /* 0 */
+} ic_cache_move;
+size_t ic_attn_weight_add_workspace(int32_t B, int32_t Tq, int32_t k_sel, int32_t Lk);
+ic_status ic_attn_weight_add(int32_t B, int32_t Tq, int32_t k_sel, int32_t Lk, const float *probs, const int32_t *idx,
+                             const float *weight_in, float *weight, void *workspace, size_t workspace_bytes, void *stream);
+size_t ic_evict_keep_workspace(int32_t B, int32_t Lk);
+ic_status ic_evict_keep(int32_t B, int32_t Lk, const float *weight, const int32_t *seq_lens, int32_t n_keep, int32_t n_first,
+                        int32_t n_recent, int32_t *keep, int32_t *keep_lens, float *keep_weight, void *workspace,
+                        size_t workspace_bytes, void *stream);
+ic_status ic_cache_compact(const ic_cache_move *caches, int32_t n_caches, int32_t B, int32_t Lk, int32_t n_keep, const int32_t *keep,
+                           const ic_paged_cache *src_pc, const ic_paged_cache *dst_pc, void *stream);
+
 /* Host-only helpers for the pattern string c = c_1..c_N in {F,S}^N (Sec. 3 Overview). */
 ic_status ic_pattern_from_string(const char *fs, uint8_t *full_mask, int32_t n);
 /* Uniform interleave: F at layers l with l % r == 0, "FSSSFSSS.." for r = 4 (Sec. 3.1). */

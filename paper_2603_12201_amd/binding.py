@@ -35,6 +35,16 @@ class PagedCache(C.Structure):
     _fields_ = [("page_size", C.c_int32), ("max_pages", C.c_int32), ("page_table", C.c_void_p), ("seq_lens", C.c_void_p)]
 
 
+class Kv4Desc(C.Structure):
+    _fields_ = [("B", C.c_int32), ("Tn", C.c_int32), ("Lk", C.c_int32), ("reserved", C.c_int32),
+                ("pos0", C.c_int64), ("pool_rows", C.c_int64)]
+
+
+class CacheMove(C.Structure):
+    _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("src_rows", C.c_int64), ("dst_rows", C.c_int64),
+                ("row_bytes", C.c_int32), ("reserved", C.c_int32)]
+
+
 class Layer(C.Structure):
     _fields_ = [("ix", IndexerDesc), ("q", C.c_void_p), ("k", C.c_void_p), ("w", C.c_void_p),
                 ("at", AttnDesc), ("Q", C.c_void_p), ("KV", C.c_void_p), ("O", C.c_void_p)]
@@ -109,6 +119,26 @@ def lib():
         L.ic_distill_loss_workspace.argtypes = [C.c_int64]
         L.ic_distill_loss.restype = C.c_int
         L.ic_distill_loss.argtypes = [C.POINTER(vp), i32, vp, C.c_int64, i32, vp, vp, vp, vp, sz, vp]
+        L.ic_kv4_write.restype = C.c_int
+        L.ic_kv4_write.argtypes = [C.POINTER(Kv4Desc), C.POINTER(PagedCache), vp, vp, vp]
+        L.ic_kv4_read.restype = C.c_int
+        L.ic_kv4_read.argtypes = [C.POINTER(Kv4Desc), C.POINTER(PagedCache), vp, vp, vp]
+        L.ic_sparse_attn_kv4_workspace.restype = sz
+        L.ic_sparse_attn_kv4_workspace.argtypes = [C.POINTER(AttnDesc)]
+        L.ic_sparse_attn_kv4.restype = C.c_int
+        L.ic_sparse_attn_kv4.argtypes = [C.POINTER(AttnDesc), C.POINTER(PagedCache), C.c_int64, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.ic_attn_probs_kv4.restype = C.c_int
+        L.ic_attn_probs_kv4.argtypes = [C.POINTER(AttnDesc), C.POINTER(PagedCache), C.c_int64, vp, vp, vp, vp, vp, vp]
+        L.ic_attn_weight_add_workspace.restype = sz
+        L.ic_attn_weight_add_workspace.argtypes = [i32, i32, i32, i32]
+        L.ic_attn_weight_add.restype = C.c_int
+        L.ic_attn_weight_add.argtypes = [i32, i32, i32, i32, vp, vp, vp, vp, vp, sz, vp]
+        L.ic_evict_keep_workspace.restype = sz
+        L.ic_evict_keep_workspace.argtypes = [i32, i32]
+        L.ic_evict_keep.restype = C.c_int
+        L.ic_evict_keep.argtypes = [i32, i32, vp, vp, i32, i32, i32, vp, vp, vp, vp, sz, vp]
+        L.ic_cache_compact.restype = C.c_int
+        L.ic_cache_compact.argtypes = [C.POINTER(CacheMove), i32, i32, i32, i32, vp, C.POINTER(PagedCache), C.POINTER(PagedCache), vp]
         L.ic_pattern_search_dp.restype = C.c_int
         L.ic_pattern_search_dp.argtypes = [C.POINTER(C.c_double), i32, i32, C.c_char_p, C.POINTER(C.c_double)]
         L.ic_topk_overlap_workspace.restype = sz
@@ -528,6 +558,199 @@ def distill_loss(probs, sel_scores, want_grad=False, workspace=None, stream=None
     _check(lib().ic_distill_loss(ptrs, len(probs), _ptr(sel_scores), nq, k_sel, _ptr(lm), _ptr(la), _ptr(grad),
                                  _ptr(workspace), workspace.numel(), _stream(stream)))
     return (lm, la, grad) if want_grad else (lm, la)
+
+
+KV4_ROW_BYTES = 400
+
+
+def _on(stream):
+    """The context in which what a call allocates belongs to its stream (None: the current one)."""
+    import contextlib
+    import torch
+    return torch.cuda.stream(stream) if isinstance(stream, torch.cuda.Stream) else contextlib.nullcontext()
+
+
+def _same_device(like, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != like.device:
+            raise IcError(Status.ERR_SHAPE, "%s is on %s, not on %s" % (name, t.device, like.device))
+
+
+def _kv4_cache(kv4, B, Lk, pc):
+    """Checks a 4-bit cache against its layout; returns (Lk, rows that it holds)."""
+    import torch
+    _need(kv4, "kv4", torch.uint8)
+    if kv4.dim() < 2 or kv4.shape[-1] != KV4_ROW_BYTES:
+        raise IcError(Status.ERR_SHAPE, "kv4 %s must have rows of %d bytes" % (tuple(kv4.shape), KV4_ROW_BYTES))
+    paged = pc is not None and bool(pc.page_table)
+    if pc is not None:
+        lens, table = pc._keep
+        if (lens is not None and lens.shape[0] != B) or (table is not None and table.shape[0] != B):
+            raise IcError(Status.ERR_SHAPE, "seq_lens / page_table are not for %d sequences" % B)
+        _same_device(kv4, seq_lens=lens, page_table=table)
+    if not paged and (kv4.dim() != 3 or kv4.shape[0] != B):
+        raise IcError(Status.ERR_SHAPE, "kv4 %s must be [%d, Lk, %d] without a page table" % (tuple(kv4.shape), B, KV4_ROW_BYTES))
+    if Lk is None:
+        if paged:
+            raise IcError(Status.ERR_SHAPE, "Lk, the bound on the sequence lengths, has to be given with a page table")
+        Lk = kv4.shape[1]
+    elif not paged and kv4.shape[1] != Lk:
+        raise IcError(Status.ERR_SHAPE, "Lk=%d but kv4 has %d positions" % (Lk, kv4.shape[1]))
+    return Lk, kv4.numel() // KV4_ROW_BYTES
+
+
+def _ref(pc):
+    return None if pc is None else C.byref(pc)
+
+
+def kv4_write(rows, kv4, pos0=0, Lk=None, pc=None, stream=None):
+    """ic_kv4_write: rows [B,Tn,576] bf16 into the 4-bit cache kv4 ([B,Lk,400] uint8, or a pool [rows,400] behind pc's page
+    table, then with Lk), at positions pos0 .., or the last Tn of pc's seq_lens."""
+    import torch
+    _need(rows, "rows", torch.bfloat16, 3)
+    B, Tn, width = rows.shape
+    if width != 576:
+        raise IcError(Status.ERR_UNSUPPORTED, "rows of %d elements (576)" % width)
+    Lk, n = _kv4_cache(kv4, B, Lk, pc)
+    _same_device(kv4, rows=rows)
+    d = Kv4Desc(B, Tn, Lk, 0, pos0, n)
+    _check(lib().ic_kv4_write(C.byref(d), _ref(pc), _ptr(rows), _ptr(kv4), _stream(stream)))
+    return kv4
+
+
+def kv4_read(kv4, B, Tn, pos0=0, Lk=None, pc=None, stream=None, out=None):
+    """ic_kv4_read: the bf16 rows [B,Tn,576] that the cache holds at positions pos0 .., or at the last Tn of pc's seq_lens."""
+    import torch
+    Lk, n = _kv4_cache(kv4, B, Lk, pc)
+    if out is None:
+        with _on(stream):
+            out = torch.empty((B, Tn, 576), dtype=torch.bfloat16, device=kv4.device)
+    _need(out, "out", torch.bfloat16, 3)
+    if tuple(out.shape) != (B, Tn, 576):
+        raise IcError(Status.ERR_SHAPE, "out %s must be %s" % (tuple(out.shape), (B, Tn, 576)))
+    _same_device(kv4, out=out)
+    d = Kv4Desc(B, Tn, Lk, 0, pos0, n)
+    _check(lib().ic_kv4_read(C.byref(d), _ref(pc), _ptr(kv4), _ptr(out), _stream(stream)))
+    return out
+
+
+def _kv4_attn_desc(Q, kv4, idx, sm_scale, Lk, pc):
+    import torch
+    _need(Q, "Q", torch.bfloat16, 4)
+    _need(idx, "idx", torch.int32, 3)
+    B, Tq, Hq, d_qk = Q.shape
+    if idx.shape[0] != B or idx.shape[1] != Tq:
+        raise IcError(Status.ERR_SHAPE, "Q %s and idx %s disagree" % (tuple(Q.shape), tuple(idx.shape)))
+    Lk, n = _kv4_cache(kv4, B, Lk, pc)
+    _same_device(kv4, Q=Q, idx=idx)
+    return AttnDesc(B, Tq, Lk, Hq, d_qk, 512, 0, 576, idx.shape[2], sm_scale), n
+
+
+def sparse_attn_kv4(Q, kv4, idx, sm_scale, Lk=None, pc=None, want_lse=False, workspace=None, stream=None, out=None):
+    """ic_sparse_attn_kv4: O [B,Tq,H_q,512] bf16 (and lse [B,Tq,H_q] fp32 if want_lse) from a 4-bit cache as kv4_write fills it."""
+    import torch
+    d, n = _kv4_attn_desc(Q, kv4, idx, sm_scale, Lk, pc)
+    with _on(stream):
+        if workspace is None:
+            workspace = _workspace(lib().ic_sparse_attn_kv4_workspace(C.byref(d)), Q)
+        O = out if out is not None else torch.empty((d.B, d.Tq, d.H_q, 512), dtype=torch.bfloat16, device=Q.device)
+        lse = torch.empty((d.B, d.Tq, d.H_q), dtype=torch.float32, device=Q.device) if want_lse else None
+    _need(O, "out", torch.bfloat16, 4)
+    if tuple(O.shape) != (d.B, d.Tq, d.H_q, 512):
+        raise IcError(Status.ERR_SHAPE, "out %s must be %s" % (tuple(O.shape), (d.B, d.Tq, d.H_q, 512)))
+    _same_device(kv4, out=O, workspace=workspace)
+    _check(lib().ic_sparse_attn_kv4(C.byref(d), _ref(pc), n, _ptr(Q), _ptr(kv4), _ptr(idx), _ptr(O), _ptr(lse), _ptr(workspace),
+                                    workspace.numel() * workspace.element_size(), _stream(stream)))
+    return (O, lse) if want_lse else O
+
+
+def attn_probs_kv4(Q, kv4, idx, sm_scale, lse, Lk=None, pc=None, stream=None):
+    """ic_attn_probs_kv4: head-averaged attention probabilities over the selected rows of a 4-bit cache, [B,Tq,k_sel] fp32.
+    lse: what sparse_attn_kv4(..., want_lse=True) returned for the same Q, kv4, idx."""
+    import torch
+    d, n = _kv4_attn_desc(Q, kv4, idx, sm_scale, Lk, pc)
+    _need(lse, "lse", torch.float32, 3)
+    if tuple(lse.shape) != (d.B, d.Tq, d.H_q):
+        raise IcError(Status.ERR_SHAPE, "lse %s must be %s" % (tuple(lse.shape), (d.B, d.Tq, d.H_q)))
+    _same_device(kv4, lse=lse)
+    with _on(stream):
+        probs = torch.empty(tuple(idx.shape), dtype=torch.float32, device=Q.device)
+    _check(lib().ic_attn_probs_kv4(C.byref(d), _ref(pc), n, _ptr(Q), _ptr(kv4), _ptr(idx), _ptr(lse), _ptr(probs), _stream(stream)))
+    return probs
+
+
+def attn_weight_add(probs, idx, weight, out=None, workspace=None, stream=None):
+    """ic_attn_weight_add: weight [B,Lk] fp32 plus what probs [B,Tq,k_sel] gave each position that idx names.  Into `out` if
+    given, else in place; returns the sum."""
+    import torch
+    _need(probs, "probs", torch.float32, 3)
+    _need(idx, "idx", torch.int32, 3)
+    _need(weight, "weight", torch.float32, 2)
+    out = weight if out is None else out
+    _need(out, "out", torch.float32, 2)
+    B, Tq, k = probs.shape
+    if tuple(idx.shape) != (B, Tq, k) or weight.shape[0] != B or out.shape != weight.shape:
+        raise IcError(Status.ERR_SHAPE, "probs %s, idx %s, weight %s, out %s disagree" % (tuple(probs.shape), tuple(idx.shape), tuple(weight.shape), tuple(out.shape)))
+    _same_device(weight, probs=probs, idx=idx, out=out, workspace=workspace)
+    Lk = weight.shape[1]
+    if workspace is None:
+        with _on(stream):
+            workspace = _workspace(lib().ic_attn_weight_add_workspace(B, Tq, k, Lk), weight)
+    _check(lib().ic_attn_weight_add(B, Tq, k, Lk, _ptr(probs), _ptr(idx), _ptr(weight), _ptr(out), _ptr(workspace),
+                                    workspace.numel() * workspace.element_size(), _stream(stream)))
+    return out
+
+
+def evict_keep(weight, n_keep, n_first=0, n_recent=0, seq_lens=None, workspace=None, stream=None):
+    """ic_evict_keep: which positions of each sequence stay.  weight [B,Lk] fp32.  Returns keep [B,n_keep] int32 (ascending,
+    -1 tail), their numbers [B] int32 (the new seq_lens) and their weights [B,n_keep] fp32."""
+    import torch
+    _need(weight, "weight", torch.float32, 2)
+    B, Lk = weight.shape
+    if seq_lens is not None:
+        _need(seq_lens, "seq_lens", torch.int32, 1)
+        if seq_lens.shape[0] != B:
+            raise IcError(Status.ERR_SHAPE, "seq_lens is not for %d sequences" % B)
+    _same_device(weight, seq_lens=seq_lens, workspace=workspace)
+    if n_keep <= 0:
+        raise IcError(Status.ERR_SHAPE, "n_keep=%d must be positive" % n_keep)
+    with _on(stream):
+        if workspace is None:
+            workspace = _workspace(lib().ic_evict_keep_workspace(B, Lk), weight)
+        keep = torch.empty((B, n_keep), dtype=torch.int32, device=weight.device)
+        lens = torch.empty((B,), dtype=torch.int32, device=weight.device)
+        kept = torch.empty((B, n_keep), dtype=torch.float32, device=weight.device)
+    _check(lib().ic_evict_keep(B, Lk, _ptr(weight), _ptr(seq_lens), n_keep, n_first, n_recent, _ptr(keep), _ptr(lens), _ptr(kept),
+                               _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
+    return keep, lens, kept
+
+
+def cache_compact(caches, keep, Lk, src_pc=None, dst_pc=None, stream=None):
+    """ic_cache_compact: for each (src, dst) of `caches`, row keep[b,j] of sequence b to row j.  src [B,Lk,..] or a pool
+    [rows,..] behind src_pc's page table; dst [B,n_keep,..] or a pool behind dst_pc's."""
+    import torch
+    _need(keep, "keep", torch.int32, 2)
+    B, n_keep = keep.shape
+    moves = (CacheMove * max(len(caches), 1))()
+    for pc, name in ((src_pc, "src_pc"), (dst_pc, "dst_pc")):
+        if pc is not None and pc._keep[1] is not None:
+            if pc._keep[1].shape[0] != B:
+                raise IcError(Status.ERR_SHAPE, "%s's page table is not for %d sequences" % (name, B))
+            _same_device(keep, page_table=pc._keep[1])
+    sp, dp = src_pc is not None and bool(src_pc.page_table), dst_pc is not None and bool(dst_pc.page_table)
+    for m, (src, dst) in zip(moves, caches):
+        _need(src, "src")
+        _need(dst, "dst")
+        _same_device(keep, src=src, dst=dst)
+        rs, rd = (1 if sp else 2), (1 if dp else 2)                            # dims in front of a row
+        if src.dim() < rs or dst.dim() < rd or src.dtype != dst.dtype or src.shape[rs:] != dst.shape[rd:]:
+            raise IcError(Status.ERR_SHAPE, "src %s and dst %s do not hold the same rows" % (tuple(src.shape), tuple(dst.shape)))
+        if (not sp and tuple(src.shape[:2]) != (B, Lk)) or (not dp and tuple(dst.shape[:2]) != (B, n_keep)):
+            raise IcError(Status.ERR_SHAPE, "src %s and dst %s must be [%d, %d, ..] and [%d, %d, ..]" % (tuple(src.shape), tuple(dst.shape), B, Lk, B, n_keep))
+        n_src, n_dst = src.shape[:rs].numel(), dst.shape[:rd].numel()
+        row = src.element_size() * src.shape[rs:].numel()
+        m.src, m.dst, m.src_rows, m.dst_rows, m.row_bytes, m.reserved = src.data_ptr(), dst.data_ptr(), n_src, n_dst, row, 0
+    _check(lib().ic_cache_compact(moves, len(caches), B, Lk, n_keep, _ptr(keep), _ref(src_pc), _ref(dst_pc), _stream(stream)))
 
 
 def debug_indexer_scores(q, k, w, q_pos0, row0, n_rows, q_scale=None, k_scale=None, stream=None):

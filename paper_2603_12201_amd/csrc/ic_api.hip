@@ -1555,6 +1555,327 @@ ic_status ic_distill_loss(const float *const *probs, int32_t n_targets, const fl
     return IC_OK;
 }
 
+// ---- 4-bit cache -----------------------------------------------------------------------------------
+
+namespace {
+
+bool aligned(const void *p, size_t n) { return (uintptr_t)p % n == 0; }
+
+ic_status check_kv4_cache(const ic_paged_cache *pc, int64_t B, int32_t Lk, int64_t pool_rows)
+{
+    if (pool_rows <= 0 || pool_rows > INT32_MAX) return fail(IC_ERR_SHAPE, "pool_rows=%lld must be in [1, 2^31)", (long long)pool_rows);
+    if (pc) {
+        ic_status s = check_paged(pc, Lk);
+        if (s != IC_OK) return s;
+    }
+    if (!(pc && pc->page_table) && B * (int64_t)Lk > pool_rows)
+        return fail(IC_ERR_SHAPE, "a dense cache of %lld x %d rows has only %lld", (long long)B, Lk, (long long)pool_rows);
+    return IC_OK;
+}
+
+ic_status kv4_rows(const ic_kv4_desc *d, const ic_paged_cache *pc, ic::Kv4RowsArgs *a)
+{
+    if (!d) return fail(IC_ERR_NULL, "4-bit cache descriptor is NULL");
+    if (d->B <= 0 || d->Tn <= 0 || d->Lk <= 0) return fail(IC_ERR_SHAPE, "4-bit cache sizes must be positive (B=%d Tn=%d Lk=%d)", d->B, d->Tn, d->Lk);
+    if (d->reserved != 0) return fail(IC_ERR_UNSUPPORTED, "reserved must be 0");
+    if ((int64_t)d->B * d->Tn > INT32_MAX) return fail(IC_ERR_SHAPE, "B*Tn too large");
+    if (d->pos0 < -((int64_t)1 << 40) || d->pos0 > ((int64_t)1 << 40)) return fail(IC_ERR_SHAPE, "pos0 out of range");
+    ic_status s = check_kv4_cache(pc, d->B, d->Lk, d->pool_rows);
+    if (s != IC_OK) return s;
+    memset(a, 0, sizeof *a);
+    a->pool_rows = d->pool_rows;
+    a->pos0 = d->pos0;
+    a->B = d->B;
+    a->Tn = d->Tn;
+    a->Lk = d->Lk;
+    a->pv = paged_view(pc);
+    return IC_OK;
+}
+
+ic_status check_attn_kv4(const ic_attn_desc *d, const ic_paged_cache *pc, int64_t pool_rows)
+{
+    ic_status s = check_attn(d);
+    if (s != IC_OK) return s;
+    if (d->d_qk != 576 || d->d_v != 512 || d->v_off != 0 || d->row_elems != 576)
+        return fail(IC_ERR_UNSUPPORTED, "a 4-bit cache holds rows of 576 with values 0..511 (d_qk=%d d_v=%d v_off=%d row_elems=%d)", d->d_qk, d->d_v,
+                    d->v_off, d->row_elems);
+    return check_kv4_cache(pc, d->B, d->Lk, pool_rows);
+}
+
+// Splits of a query.  A workgroup's four waves take a split together (their tiles meet in LDS) unless the queries alone give
+// every wave of the chip one of its own.
+struct Kv4Splits {
+    int n, len;
+    bool together;
+    size_t o_bytes, bytes;
+};
+Kv4Splits kv4_splits(const ic_attn_desc *d)
+{
+    const int64_t nq = (int64_t)d->B * d->Tq, tiles = (d->k_sel + 31) / 32;
+    Kv4Splits r = {1, (int)tiles * 32, nq < 1024, 0, 0};
+    if (nq < 256) {
+        int64_t ns = 256 / nq, most = (tiles + 3) / 4;
+        if (ns > most) ns = most;
+        const int64_t per = (tiles + ns - 1) / ns;
+        r.len = (int)per * 32;
+        r.n = (int)((tiles + per - 1) / per);
+    }
+    if (r.n > 1) {
+        r.o_bytes = align_up((size_t)nq * r.n * d->H_q * d->d_v * 4);
+        r.bytes = r.o_bytes + align_up((size_t)nq * r.n * d->H_q * 8);
+    }
+    return r;
+}
+
+ic::Kv4AttnArgs kv4_attn_args(const ic_attn_desc *d, const ic_paged_cache *pc, int64_t pool_rows, const void *Q, const void *KV4, const int32_t *idx)
+{
+    ic::Kv4AttnArgs a;
+    memset(&a, 0, sizeof a);
+    a.Q = Q;
+    a.KV4 = KV4;
+    a.idx = idx;
+    a.pool_rows = pool_rows;
+    a.B = d->B;
+    a.Tq = d->Tq;
+    a.Lk = d->Lk;
+    a.H_q = d->H_q;
+    a.k_sel = d->k_sel;
+    a.scale_log2e = d->sm_scale * 1.4426950408889634f;
+    a.pv = paged_view(pc);
+    return a;
+}
+
+} // namespace
+
+ic_status ic_kv4_write(const ic_kv4_desc *d, const ic_paged_cache *pc, const void *rows, void *KV4, void *stream)
+{
+    ic::Kv4RowsArgs a;
+    ic_status s = kv4_rows(d, pc, &a);
+    if (s != IC_OK) return s;
+    if (!rows || !KV4) return fail(IC_ERR_NULL, "rows and KV4 must not be NULL");
+    if (!aligned(rows, 16) || !aligned(KV4, 16)) return fail(IC_ERR_SHAPE, "rows and KV4 must be 16-byte aligned");
+    a.rows = rows;
+    a.kv4 = KV4;
+    hipError_t e = ic::launch_kv4_write(a, (hipStream_t)stream);
+    if (e != hipSuccess) return fail(IC_ERR_HIP, "4-bit write launch failed: %s", hipGetErrorString(e));
+    return IC_OK;
+}
+
+ic_status ic_kv4_read(const ic_kv4_desc *d, const ic_paged_cache *pc, const void *KV4, void *rows, void *stream)
+{
+    ic::Kv4RowsArgs a;
+    ic_status s = kv4_rows(d, pc, &a);
+    if (s != IC_OK) return s;
+    if (!rows || !KV4) return fail(IC_ERR_NULL, "rows and KV4 must not be NULL");
+    if (!aligned(rows, 16) || !aligned(KV4, 16)) return fail(IC_ERR_SHAPE, "rows and KV4 must be 16-byte aligned");
+    a.kv4 = const_cast<void *>(KV4);
+    a.out = rows;
+    hipError_t e = ic::launch_kv4_read(a, (hipStream_t)stream);
+    if (e != hipSuccess) return fail(IC_ERR_HIP, "4-bit read launch failed: %s", hipGetErrorString(e));
+    return IC_OK;
+}
+
+size_t ic_sparse_attn_kv4_workspace(const ic_attn_desc *d)
+{
+    if (check_attn_kv4(d, nullptr, INT32_MAX) != IC_OK && check_attn(d) != IC_OK) return 0;
+    return kv4_splits(d).bytes;
+}
+
+ic_status ic_sparse_attn_kv4(const ic_attn_desc *d, const ic_paged_cache *pc, int64_t pool_rows, const void *Q, const void *KV4,
+                             const int32_t *idx, void *O, float *lse, void *workspace, size_t workspace_bytes, void *stream)
+{
+    ic_status s = check_attn_kv4(d, pc, pool_rows);
+    if (s != IC_OK) return s;
+    if (!Q || !KV4 || !idx || !O) return fail(IC_ERR_NULL, "Q, KV4, idx and O must not be NULL");
+    if (!aligned(Q, 16) || !aligned(KV4, 16) || !aligned(O, 16)) return fail(IC_ERR_SHAPE, "Q, KV4 and O must be 16-byte aligned");
+    const Kv4Splits sp = kv4_splits(d);
+    s = check_ws(workspace, workspace_bytes, sp.bytes);
+    if (s != IC_OK) return s;
+    ic::Kv4AttnArgs a = kv4_attn_args(d, pc, pool_rows, Q, KV4, idx);
+    a.O = O;
+    a.lse = lse;
+    a.n_splits = sp.n;
+    a.split_len = sp.len;
+    if (sp.n > 1) {
+        a.part_o = workspace;
+        a.part_ml = (float *)((char *)workspace + sp.o_bytes);
+    }
+    const hipStream_t st = (hipStream_t)stream;
+    hipError_t e;
+    {
+        ProfScope ps(2, st);
+        e = ic::launch_kv4_attn(a, sp.together, st);
+    }
+    if (e != hipSuccess) return fail(IC_ERR_HIP, "4-bit attention launch failed: %s", hipGetErrorString(e));
+    if (sp.n > 1) {
+        ic::AttnArgs m;
+        memset(&m, 0, sizeof m);
+        m.O = m.Os[0] = O;
+        m.lse = lse;
+        m.part_o = a.part_o;
+        m.part_ml = a.part_ml;
+        m.part_wide = 1;
+        m.B = d->B;
+        m.Tq = d->Tq;
+        m.H_q = d->H_q;
+        m.n_layers = 1;
+        m.n_splits = sp.n;
+        ProfScope ps(3, st);
+        e = ic::launch_attn_merge(m, d->d_v, st);
+        if (e != hipSuccess) return fail(IC_ERR_HIP, "split merge launch failed: %s", hipGetErrorString(e));
+    }
+    return IC_OK;
+}
+
+ic_status ic_attn_probs_kv4(const ic_attn_desc *d, const ic_paged_cache *pc, int64_t pool_rows, const void *Q, const void *KV4,
+                            const int32_t *idx, const float *lse, float *probs, void *stream)
+{
+    ic_status s = check_attn_kv4(d, pc, pool_rows);
+    if (s != IC_OK) return s;
+    if (!Q || !KV4 || !idx || !lse || !probs) return fail(IC_ERR_NULL, "Q, KV4, idx, lse and probs must not be NULL");
+    if (!aligned(Q, 16) || !aligned(KV4, 16)) return fail(IC_ERR_SHAPE, "Q and KV4 must be 16-byte aligned");
+    ic::Kv4AttnArgs a = kv4_attn_args(d, pc, pool_rows, Q, KV4, idx);
+    a.lse = const_cast<float *>(lse);
+    a.probs = probs;
+    const Kv4Splits sp = kv4_splits(d);
+    a.n_splits = sp.n;
+    a.split_len = sp.len;
+    hipError_t e = ic::launch_kv4_probs(a, (hipStream_t)stream);
+    if (e != hipSuccess) return fail(IC_ERR_HIP, "4-bit attention-probability launch failed: %s", hipGetErrorString(e));
+    return IC_OK;
+}
+
+// ---- eviction --------------------------------------------------------------------------------------
+
+namespace {
+
+ic_status weight_args(int32_t B, int32_t Tq, int32_t k_sel, int32_t Lk, ic::WeightArgs *a, size_t *ws)
+{
+    if (B <= 0 || Tq <= 0 || k_sel <= 0 || Lk <= 0) return fail(IC_ERR_SHAPE, "weight sizes must be positive (B=%d Tq=%d k_sel=%d Lk=%d)", B, Tq, k_sel, Lk);
+    if (B > 65535) return fail(IC_ERR_UNSUPPORTED, "B=%d exceeds 65535", B);
+    if ((int64_t)B * Tq > INT32_MAX || (int64_t)B * Lk > INT32_MAX) return fail(IC_ERR_SHAPE, "B*Tq or B*Lk too large");
+    memset(a, 0, sizeof *a);
+    a->B = B;
+    a->Tq = Tq;
+    a->k_sel = k_sel;
+    a->Lk = Lk;
+    ic::weight_plan(*a);
+    *ws = a->n_chunks > 1 ? align_up((size_t)B * a->n_chunks * Lk * 8) : 0;
+    return IC_OK;
+}
+
+} // namespace
+
+size_t ic_attn_weight_add_workspace(int32_t B, int32_t Tq, int32_t k_sel, int32_t Lk)
+{
+    ic::WeightArgs a;
+    size_t ws = 0;
+    return weight_args(B, Tq, k_sel, Lk, &a, &ws) == IC_OK ? ws : 0;
+}
+
+ic_status ic_attn_weight_add(int32_t B, int32_t Tq, int32_t k_sel, int32_t Lk, const float *probs, const int32_t *idx,
+                             const float *weight_in, float *weight, void *workspace, size_t workspace_bytes, void *stream)
+{
+    ic::WeightArgs a;
+    size_t ws = 0;
+    ic_status s = weight_args(B, Tq, k_sel, Lk, &a, &ws);
+    if (s != IC_OK) return s;
+    if (!probs || !idx || !weight) return fail(IC_ERR_NULL, "probs, idx and weight must not be NULL");
+    s = check_ws(workspace, workspace_bytes, ws);
+    if (s != IC_OK) return s;
+    a.probs = probs;
+    a.idx = idx;
+    a.in = weight_in;
+    a.out = weight;
+    a.part = (unsigned long long *)workspace;
+    hipError_t e = ic::launch_weight_add(a, (hipStream_t)stream);
+    if (e != hipSuccess) return fail(IC_ERR_HIP, "weight launch failed: %s", hipGetErrorString(e));
+    return IC_OK;
+}
+
+size_t ic_evict_keep_workspace(int32_t B, int32_t Lk)
+{
+    (void)B;
+    (void)Lk;
+    return 0;
+}
+
+ic_status ic_evict_keep(int32_t B, int32_t Lk, const float *weight, const int32_t *seq_lens, int32_t n_keep, int32_t n_first,
+                        int32_t n_recent, int32_t *keep, int32_t *keep_lens, float *keep_weight, void *workspace,
+                        size_t workspace_bytes, void *stream)
+{
+    if (B <= 0 || Lk <= 0 || n_keep <= 0 || n_first < 0 || n_recent < 0)
+        return fail(IC_ERR_SHAPE, "eviction sizes: B=%d Lk=%d n_keep=%d must be positive, n_first=%d n_recent=%d not negative", B, Lk, n_keep, n_first, n_recent);
+    if (n_keep > Lk || (int64_t)n_first + n_recent > n_keep)
+        return fail(IC_ERR_SHAPE, "need n_first + n_recent <= n_keep <= Lk (%d + %d, %d, %d)", n_first, n_recent, n_keep, Lk);
+    if ((int64_t)B * Lk > INT32_MAX) return fail(IC_ERR_SHAPE, "B*Lk too large");
+    if (!weight || !keep || !keep_lens) return fail(IC_ERR_NULL, "weight, keep and keep_lens must not be NULL");
+    ic_status s = check_ws(workspace, workspace_bytes, ic_evict_keep_workspace(B, Lk));
+    if (s != IC_OK) return s;
+    ic::EvictArgs a;
+    memset(&a, 0, sizeof a);
+    a.weight = weight;
+    a.seq_lens = seq_lens;
+    a.keep = keep;
+    a.lens = keep_lens;
+    a.kept = keep_weight;
+    a.B = B;
+    a.Lk = Lk;
+    a.n_keep = n_keep;
+    a.n_first = n_first;
+    a.n_recent = n_recent;
+    hipError_t e = ic::launch_evict_keep(a, (hipStream_t)stream);
+    if (e != hipSuccess) return fail(IC_ERR_HIP, "eviction launch failed: %s", hipGetErrorString(e));
+    return IC_OK;
+}
+
+ic_status ic_cache_compact(const ic_cache_move *caches, int32_t n_caches, int32_t B, int32_t Lk, int32_t n_keep, const int32_t *keep,
+                           const ic_paged_cache *src_pc, const ic_paged_cache *dst_pc, void *stream)
+{
+    if (!caches || !keep) return fail(IC_ERR_NULL, "caches and keep must not be NULL");
+    if (n_caches < 1 || n_caches > IC_MAX_MOVE_CACHES) return fail(IC_ERR_SHAPE, "n_caches=%d must be in [1, %d]", n_caches, IC_MAX_MOVE_CACHES);
+    if (B <= 0 || Lk <= 0 || n_keep <= 0 || n_keep > Lk) return fail(IC_ERR_SHAPE, "need B > 0 and 0 < n_keep <= Lk (B=%d n_keep=%d Lk=%d)", B, n_keep, Lk);
+    if ((int64_t)B * Lk > INT32_MAX) return fail(IC_ERR_SHAPE, "B*Lk too large");
+    const bool sp = src_pc && src_pc->page_table, dp = dst_pc && dst_pc->page_table;
+    if (sp) {
+        ic_status s = check_paged(src_pc, Lk);
+        if (s != IC_OK) return s;
+    }
+    if (dp) {
+        ic_status s = check_paged(dst_pc, n_keep);
+        if (s != IC_OK) return s;
+    }
+    ic::CompactArgs a;
+    memset(&a, 0, sizeof a);
+    for (int i = 0; i < n_caches; ++i) {
+        const ic_cache_move &c = caches[i];
+        if (!c.src || !c.dst) return fail(IC_ERR_NULL, "cache %d: src and dst must not be NULL", i);
+        if (c.reserved != 0) return fail(IC_ERR_UNSUPPORTED, "reserved must be 0");
+        if (c.row_bytes <= 0 || c.row_bytes % 4 != 0 || c.row_bytes > (1 << 20) || !aligned(c.src, 4) || !aligned(c.dst, 4))
+            return fail(IC_ERR_SHAPE, "cache %d: rows of %d bytes (a multiple of 4, 4-byte aligned)", i, c.row_bytes);
+        if (c.src_rows <= 0 || c.dst_rows <= 0 || (!sp && c.src_rows < (int64_t)B * Lk) || (!dp && c.dst_rows < (int64_t)B * n_keep))
+            return fail(IC_ERR_SHAPE, "cache %d: src_rows=%lld dst_rows=%lld do not hold the sequences", i, (long long)c.src_rows, (long long)c.dst_rows);
+        const Range s = {(const char *)c.src, (size_t)c.src_rows * c.row_bytes}, d = {(const char *)c.dst, (size_t)c.dst_rows * c.row_bytes};
+        const bool pages = sp && dp && c.src == c.dst && src_pc->page_table != dst_pc->page_table;
+        if (s.meets(d) && !pages) return fail(IC_ERR_SHAPE, "cache %d: src and dst overlap", i);
+        a.src[i] = (const unsigned char *)c.src;
+        a.dst[i] = (unsigned char *)c.dst;
+        a.row_bytes[i] = c.row_bytes;
+        a.src_rows[i] = c.src_rows;
+        a.dst_rows[i] = c.dst_rows;
+    }
+    a.keep = keep;
+    a.n_caches = n_caches;
+    a.B = B;
+    a.Lk = Lk;
+    a.n_keep = n_keep;
+    a.sv = paged_view(sp ? src_pc : nullptr);
+    a.dv = paged_view(dp ? dst_pc : nullptr);
+    hipError_t e = ic::launch_compact(a, (hipStream_t)stream);
+    if (e != hipSuccess) return fail(IC_ERR_HIP, "compaction launch failed: %s", hipGetErrorString(e));
+    return IC_OK;
+}
+
 size_t ic_topk_overlap_workspace(int32_t n_layers)
 {
     if (n_layers <= 0 || n_layers > IC_MAX_OVERLAP_LAYERS) return 0;

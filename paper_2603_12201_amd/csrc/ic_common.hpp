@@ -2,6 +2,7 @@
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include <type_traits>
 
 #include "indexcache.h"
 
@@ -199,6 +200,66 @@ struct DistillArgs {
     float *grad;          // [nq, k_sel] or nullptr
 };
 
+// Rows of a 4-bit cache, written from (rows) or read back to (out) bf16.
+struct Kv4RowsArgs {
+    const void *rows;     // [B,Tn,576] bf16
+    void *kv4;            // [B,Lk,400 bytes] or the page pool
+    void *out;            // [B,Tn,576] bf16
+    int64_t pool_rows;    // rows that kv4 holds
+    int64_t pos0;         // position of the first row (no seq_lens)
+    int32_t B, Tn, Lk;
+    PagedView pv;
+};
+
+// Sparse attention over a 4-bit cache, or the selected rows' weights.
+struct Kv4AttnArgs {
+    const void *Q;        // [B,Tq,H_q,576] bf16
+    const void *KV4;
+    const int32_t *idx;   // [B,Tq,k_sel]
+    void *O;              // [B,Tq,H_q,512] bf16
+    float *lse;           // [B,Tq,H_q] or nullptr; read for probs
+    float *probs;         // [B,Tq,k_sel]
+    void *part_o;         // [B*Tq, n_splits, H_q, 512] fp32, each normalised by its own row sum
+    float *part_ml;       // [B*Tq, n_splits, H_q, 2] fp32 (maximum in log2 units, sum)
+    int64_t pool_rows;
+    int32_t B, Tq, Lk, H_q, k_sel;
+    int32_t n_splits, split_len;   // slots per split, a multiple of 32
+    float scale_log2e;
+    PagedView pv;
+};
+
+// Weights of the positions, summed over the query rows.
+struct WeightArgs {
+    const float *probs;   // [B,Tq,k_sel]
+    const int32_t *idx;   // [B,Tq,k_sel]
+    const float *in;      // [B,Lk] or nullptr
+    float *out;           // [B,Lk], may be `in`
+    unsigned long long *part;   // [B][chunks][Lk] sums of the chunks of rows (chunks > 1)
+    int32_t B, Tq, k_sel, Lk;
+    int32_t range, n_ranges, chunk_rows, n_chunks;
+};
+
+// Which positions stay.
+struct EvictArgs {
+    const float *weight;  // [B,Lk]
+    const int32_t *seq_lens;   // [B] or nullptr
+    int32_t *keep;        // [B,n_keep]
+    int32_t *lens;        // [B]
+    float *kept;          // [B,n_keep] or nullptr
+    int32_t B, Lk, n_keep, n_first, n_recent;
+};
+
+// Rows moved to where `keep` says.
+struct CompactArgs {
+    const unsigned char *src[IC_MAX_MOVE_CACHES];
+    unsigned char *dst[IC_MAX_MOVE_CACHES];
+    int32_t row_bytes[IC_MAX_MOVE_CACHES];
+    int64_t src_rows[IC_MAX_MOVE_CACHES], dst_rows[IC_MAX_MOVE_CACHES];
+    const int32_t *keep;  // [B,n_keep]
+    int32_t n_caches, B, Lk, n_keep;
+    PagedView sv, dv;
+};
+
 // Sum over the 16 lanes of a row (lanes with equal lane / 16) on the data-parallel-primitive path:
 // shifts by 1, 2, 4, 8 lanes inside the row; lanes without a source add zero.  Lane 15 of the row
 // holds the total.
@@ -247,6 +308,14 @@ hipError_t launch_attn_probs(const ProbsArgs &a, int d_qk, hipStream_t st);
 hipError_t launch_distill(const DistillArgs &a, int64_t nq, double *loss_multi, double *loss_avg, hipStream_t st);
 hipError_t launch_calib(int kind, const void *src, void *dst, const int32_t *idx, int64_t n, int64_t table_rows, int row_bytes,
                         int wgs, hipStream_t st);
+hipError_t launch_kv4_write(const Kv4RowsArgs &a, hipStream_t st);
+hipError_t launch_kv4_read(const Kv4RowsArgs &a, hipStream_t st);
+hipError_t launch_kv4_attn(const Kv4AttnArgs &a, bool together, hipStream_t st);
+hipError_t launch_kv4_probs(const Kv4AttnArgs &a, hipStream_t st);
+void weight_plan(WeightArgs &a);
+hipError_t launch_weight_add(const WeightArgs &a, hipStream_t st);
+hipError_t launch_evict_keep(const EvictArgs &a, hipStream_t st);
+hipError_t launch_compact(const CompactArgs &a, hipStream_t st);
 bool score_shape_supported(int dtype, int H_I, int d_I);
 bool attn_shape_supported(int d_qk, int d_v);
 
