@@ -1795,9 +1795,8 @@ ic_status ic_attn_weight_add(int32_t B, int32_t Tq, int32_t k_sel, int32_t Lk, c
 
 size_t ic_evict_keep_workspace(int32_t B, int32_t Lk)
 {
-    (void)B;
-    (void)Lk;
-    return 0;
+    if (B <= 0 || Lk <= 0 || (int64_t)B * Lk > INT32_MAX) return 0;
+    return align_up(ic::evict_ws_bytes(B, Lk));
 }
 
 ic_status ic_evict_keep(int32_t B, int32_t Lk, const float *weight, const int32_t *seq_lens, int32_t n_keep, int32_t n_first,
@@ -1819,6 +1818,7 @@ ic_status ic_evict_keep(int32_t B, int32_t Lk, const float *weight, const int32_
     a.keep = keep;
     a.lens = keep_lens;
     a.kept = keep_weight;
+    a.ws = workspace;
     a.B = B;
     a.Lk = Lk;
     a.n_keep = n_keep;

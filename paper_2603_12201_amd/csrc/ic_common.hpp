@@ -246,7 +246,9 @@ struct EvictArgs {
     int32_t *keep;        // [B,n_keep]
     int32_t *lens;        // [B]
     float *kept;          // [B,n_keep] or nullptr
+    void *ws;             // evict_ws_bytes()
     int32_t B, Lk, n_keep, n_first, n_recent;
+    int32_t n_parts;      // (set by the launcher)
 };
 
 // Rows moved to where `keep` says.
@@ -314,7 +316,8 @@ hipError_t launch_kv4_attn(const Kv4AttnArgs &a, bool together, hipStream_t st);
 hipError_t launch_kv4_probs(const Kv4AttnArgs &a, hipStream_t st);
 void weight_plan(WeightArgs &a);
 hipError_t launch_weight_add(const WeightArgs &a, hipStream_t st);
-hipError_t launch_evict_keep(const EvictArgs &a, hipStream_t st);
+size_t evict_ws_bytes(int B, int Lk);
+hipError_t launch_evict_keep(EvictArgs a, hipStream_t st);
 hipError_t launch_compact(const CompactArgs &a, hipStream_t st);
 bool score_shape_supported(int dtype, int H_I, int d_I);
 bool attn_shape_supported(int d_qk, int d_v);

@@ -5,14 +5,15 @@
 //                   positions in LDS and adds there in 64-bit fixed point (units of 2^-48), so the order of the additions
 //                   does not show in the sum.  Bound by memory (probs and idx once), or for a few rows by the launch.
 //   evict_kernel    the n_keep positions of a sequence that stay: the first n_first, the last n_recent, and the largest weights
-//                   among the others (equal weights: the lower position).  Radix selection on the bits, then the positions in
-//                   order.
+//                   among the others (equal weights: the lower position).  See there.
 //   compact_kernel  rows of several caches to their new places.  Bound by memory.
 #include "ic_common.hpp"
 
 namespace ic {
 
 namespace {
+
+typedef __attribute__((ext_vector_type(2))) unsigned int u32x2;
 
 // p in [0, 1] in units of 2^-48, rounded down; what is not a number counts as 0
 __device__ __forceinline__ unsigned long long fixed48(float p)
@@ -74,91 +75,278 @@ __device__ __forceinline__ unsigned int weight_key(float w)
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// One workgroup per sequence.
-__global__ __launch_bounds__(1024) void evict_kernel(EvictArgs a)
+// ---- which positions stay -------------------------------------------------------------------------------------------
+//
+// Three digits of the keys, 11, 11 and 10 bits, from the top: a digit's histogram over the keys whose higher digits are the
+// border's says which value of it the border has and how many keys are still to be taken below; after the third the border is
+// one key, and of its positions the lowest are taken.  Keys stay in registers, 1024 apart, so a (register, wave) pair is a run
+// of 64 positions and the places of the kept ones follow from those runs' counts.
+// What positions hold most often is zero (nothing ever selected them): additions to one LDS word go one after the other, so the
+// keys of zero are counted by ballots.
+
+constexpr int kEvictThreads = 1024;
+constexpr unsigned int kZeroKey = 0x80000000u;
+
+// From `bins` (descending: bin t of this thread's digit order), the digit at which the running number reaches `left`.
+struct Digit {
+    unsigned int value, left;                 // the border's digit; how many of the keys that have it are taken
+};
+__device__ __forceinline__ Digit find_digit(const unsigned int (&n)[2], int n_bins, unsigned int left, unsigned int *sh, int tid)
 {
-    __shared__ unsigned int hist[256], wave_n[2][16];
-    __shared__ unsigned int s_prefix, s_left;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int b = blockIdx.x;
-    const int len = a.seq_lens ? max(0, min(a.seq_lens[b], a.Lk)) : a.Lk;
-    const float *w = a.weight + (int64_t)b * a.Lk;
+    // n[0]: the higher bin (n_bins - 1 - 2 t), n[1]: the one below it
+    const int lane = tid & 63, wave = tid >> 6;
+    const unsigned int own = n[0] + n[1], incl = wave_incl_scan(own);
+    if (lane == 63) sh[wave] = incl;
+    __syncthreads();
+    unsigned int before = incl - own;
+#pragma unroll
+    for (int v = 0; v < kEvictThreads / 64; ++v) before += v < wave ? sh[v] : 0u;
+    if (before < left && left <= before + own) {
+        const bool low = before + n[0] < left;
+        sh[16] = (unsigned)(n_bins - 1 - 2 * tid - (low ? 1 : 0));
+        sh[17] = left - before - (low ? n[0] : 0u);
+    }
+    __syncthreads();
+    const Digit d = {sh[16], sh[17]};
+    __syncthreads();
+    return d;
+}
+
+__device__ __forceinline__ unsigned int digit_of(unsigned int k, int level) { return level == 0 ? k >> 21 : level == 1 ? k >> 10 & 2047u : k & 1023u; }
+__device__ __forceinline__ bool same_above(unsigned int k, unsigned int border, int level)   // the digits above `level` are the border's
+{
+    return level == 0 || (level == 1 ? k >> 21 == border >> 21 : k >> 10 == border >> 10);
+}
+
+// A level's histogram of this workgroup's keys that lie in [lo, hi), from position p0.
+template <int R>
+__device__ __forceinline__ void count_digits(unsigned int *hist, const unsigned int (&key)[R], int p0, int lo, int hi, unsigned int border, int level, int tid)
+{
+    const int n_bins = level == 2 ? 1024 : 2048;
+    for (int i = tid; i < n_bins; i += kEvictThreads) hist[i] = 0;
+    __syncthreads();
+    unsigned int zeros = 0;
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+        const int i = p0 + j * kEvictThreads + tid;
+        const bool mine = i >= lo && i < hi && same_above(key[j], border, level), zero = key[j] == kZeroKey;
+        zeros += (unsigned)__popcll(__ballot(mine && zero));
+        if (mine && !zero) atomicAdd(&hist[digit_of(key[j], level)], 1u);
+    }
+    if ((tid & 63) == 0 && zeros != 0u) atomicAdd(&hist[digit_of(kZeroKey, level)], zeros);
+    __syncthreads();
+}
+
+// Writes what stays of a run of R * 1024 positions from p0: those with take_all or above the border, and of the ties the first
+// `left`, `ties0` of which lie before p0.  at0: how many positions in front of p0 stay.
+template <int R>
+__device__ __forceinline__ void emit_kept(const EvictArgs &a, int b, int p0, int lo, int hi, int len, bool any, unsigned int border, unsigned int left,
+                                          unsigned int ties0, unsigned int at0, const unsigned int (&key)[R], const float (&w)[R],
+                                          unsigned int (*runs)[2], int tid)
+{
+    const int lane = tid & 63, wave = tid >> 6;
+    constexpr int kWaves = kEvictThreads / 64, kRuns = R * kWaves;
+    const unsigned long long below = (1ull << lane) - 1;
+    // counts of the runs: {kept for certain, ties}
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+        const int i = p0 + j * kEvictThreads + tid;
+        const bool in = i < len, inner = i >= lo && i < hi;
+        const unsigned long long ma = __ballot(in && (!inner || (any && key[j] > border))), mt = __ballot(in && inner && any && key[j] == border);
+        if (lane == 0) {
+            runs[j * kWaves + wave][0] = (unsigned)__popcll(ma);
+            runs[j * kWaves + wave][1] = (unsigned)__popcll(mt);
+        }
+    }
+    __syncthreads();
+    if (wave == 0) {                           // exclusive sums over the runs, 64 at a time
+        unsigned int sa = 0, st = ties0;
+        for (int r0 = 0; r0 < kRuns; r0 += 64) {
+            const int r = r0 + lane;
+            const unsigned int na = r < kRuns ? runs[r][0] : 0u, nt = r < kRuns ? runs[r][1] : 0u;
+            const unsigned int ia = wave_incl_scan(na), it = wave_incl_scan(nt);
+            if (r < kRuns) {
+                runs[r][0] = sa + ia - na;
+                runs[r][1] = st + it - nt;
+            }
+            sa += (unsigned)__builtin_amdgcn_readlane((int)ia, 63);
+            st += (unsigned)__builtin_amdgcn_readlane((int)it, 63);
+        }
+    }
+    __syncthreads();
     int32_t *keep = a.keep + (int64_t)b * a.n_keep;
     float *kept = a.kept ? a.kept + (int64_t)b * a.n_keep : nullptr;
-    const int n = min(len, a.n_keep);
-    if (tid == 0) a.lens[b] = n;
-    for (int i = n + tid; i < a.n_keep; i += 1024) {
-        keep[i] = -1;
-        if (kept) kept[i] = 0.f;
+    const unsigned int ties_taken0 = min(ties0, left);
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+        const int i = p0 + j * kEvictThreads + tid;
+        const bool in = i < len, inner = i >= lo && i < hi;
+        const bool sure = in && (!inner || (any && key[j] > border)), tie = in && inner && any && key[j] == border;
+        const unsigned long long ma = __ballot(sure), mt = __ballot(tie);
+        const unsigned int ties = runs[j * kWaves + wave][1] + (unsigned)__popcll(mt & below);       // of the sequence, before this position
+        if (sure || (tie && ties < left)) {
+            const unsigned int at = at0 + runs[j * kWaves + wave][0] + (unsigned)__popcll(ma & below) + min(ties, left) - ties_taken0;
+            if (at < (unsigned)a.n_keep) {
+                keep[at] = i;
+                if (kept) kept[at] = w[j];
+            }
+        }
     }
-    if (len <= a.n_keep) {
-        for (int i = tid; i < n; i += 1024) {
-            keep[i] = i;
-            if (kept) kept[i] = w[i];
+}
+
+// What every form does first: the sequence's length and number, and all of the outputs where nothing has to go.
+// Returns false when nothing else is to be done.
+__device__ __forceinline__ bool evict_begin(const EvictArgs &a, int b, int part, int n_parts, bool write, int *len_out, int tid)
+{
+    const int len = a.seq_lens ? max(0, min(a.seq_lens[b], a.Lk)) : a.Lk;
+    const int n = min(len, a.n_keep);
+    *len_out = len;
+    if (write) {
+        if (tid == 0 && part == 0) a.lens[b] = n;
+        const bool all = len <= a.n_keep;
+        for (int i = (all ? 0 : n) + part * kEvictThreads + tid; i < a.n_keep; i += n_parts * kEvictThreads) {
+            const int64_t at = (int64_t)b * a.n_keep + i;
+            a.keep[at] = i < n ? i : -1;
+            if (a.kept) a.kept[at] = i < n ? a.weight[(int64_t)b * a.Lk + i] : 0.f;
+        }
+    }
+    return len > a.n_keep;
+}
+
+// One workgroup per sequence of up to R * 1024 positions.
+template <int R>
+__global__ __launch_bounds__(kEvictThreads) void evict_kernel(EvictArgs a)
+{
+    __shared__ unsigned int hist[2048], sh[32];
+    __shared__ unsigned int runs[R * kEvictThreads / 64][2];
+    const int tid = threadIdx.x, b = blockIdx.x;
+    int len;
+    if (!evict_begin(a, b, 0, 1, true, &len, tid)) return;
+    const int lo = a.n_first, hi = len - a.n_recent, want = a.n_keep - a.n_first - a.n_recent;
+    float w[R];
+    unsigned int key[R];
+#pragma unroll
+    for (int j = 0; j < R; ++j) w[j] = a.weight[(int64_t)b * a.Lk + min(j * kEvictThreads + tid, len - 1)];
+#pragma unroll
+    for (int j = 0; j < R; ++j) key[j] = weight_key(w[j]);
+    unsigned int border = 0, left = (unsigned)want;
+    if (want > 0) {
+#pragma unroll
+        for (int level = 0; level < 3; ++level) {
+            count_digits<R>(hist, key, 0, lo, hi, border, level, tid);
+            const int n_bins = level == 2 ? 1024 : 2048, bin = n_bins - 1 - 2 * tid;
+            const unsigned int n[2] = {bin > 0 ? hist[bin] : 0u, bin > 0 ? hist[bin - 1] : 0u};
+            const Digit d = find_digit(n, n_bins, left, sh, tid);
+            border |= d.value << (level == 0 ? 21 : level == 1 ? 10 : 0);
+            left = d.left;
+        }
+    }
+    emit_kept<R>(a, b, 0, lo, hi, len, want > 0, border, left, 0u, 0u, key, w, runs, tid);
+}
+
+// Longer sequences: a workgroup per 16384 positions and a launch per digit, and one that writes.  Each launch adds up the
+// workgroups' histograms of the digit before it (8 KB each) by itself.
+constexpr int kPartR = 16, kPart = kPartR * kEvictThreads;
+struct PartCounts {
+    unsigned int hist[2][2048], last[1024];
+    unsigned int above[2];                    // inner keys above the border by the first digit; by the second
+    unsigned int border[2], left[2];          // (of part 0: as the second and the third launch have found them)
+};
+
+template <int LEVEL>
+__global__ __launch_bounds__(kEvictThreads) void evict_part_kernel(EvictArgs a)
+{
+    __shared__ unsigned int hist[2048], sh[32];
+    __shared__ unsigned int runs[kPartR * kEvictThreads / 64][2];
+    __shared__ unsigned int before[2];
+    const int tid = threadIdx.x;
+    const int b = blockIdx.x / a.n_parts, part = blockIdx.x - b * a.n_parts;
+    int len;
+    if (!evict_begin(a, b, part, a.n_parts, LEVEL == 3, &len, tid)) return;
+    const int lo = a.n_first, hi = len - a.n_recent, want = a.n_keep - a.n_first - a.n_recent;
+    const int p0 = part * kPart;
+    if (p0 >= len || (LEVEL < 3 && want == 0)) return;
+    const int live = (len + kPart - 1) / kPart;                             // parts that hold positions
+    PartCounts *const seq = (PartCounts *)a.ws + (int64_t)b * a.n_parts, *const own = seq + part;
+    float w[kPartR];
+    unsigned int key[kPartR];
+#pragma unroll
+    for (int j = 0; j < kPartR; ++j) w[j] = a.weight[(int64_t)b * a.Lk + min(p0 + j * kEvictThreads + tid, len - 1)];
+    unsigned int border = 0, left = (unsigned)want;
+    if (LEVEL >= 2 && want > 0) {
+        border = seq[0].border[LEVEL - 2];
+        left = seq[0].left[LEVEL - 2];
+    }
+    if (LEVEL == 3 && tid < 2) before[tid] = 0;
+    if (LEVEL >= 1 && want > 0) {
+        // the digit of the level before: the parts' histograms together
+        constexpr int n_bins = LEVEL == 3 ? 1024 : 2048;
+        const int bin = n_bins - 1 - 2 * tid;
+        unsigned int n[2] = {0u, 0u}, front[2] = {0u, 0u};                  // of all parts; of those before this one
+        if (bin > 0) {
+#pragma unroll 8
+            for (int c = 0; c < live; ++c) {
+                const unsigned int *h = LEVEL == 3 ? seq[c].last : seq[c].hist[LEVEL - 1];
+                const u32x2 x = *(const u32x2 *)(h + bin - 1);
+                n[0] += x[1];
+                n[1] += x[0];
+                if (LEVEL == 3 && c < part) {
+                    front[0] += x[1];
+                    front[1] += x[0];
+                }
+            }
+        }
+        const Digit d = find_digit(n, n_bins, left, sh, tid);
+        border |= d.value << (LEVEL == 1 ? 21 : LEVEL == 2 ? 10 : 0);
+        left = d.left;
+        if (LEVEL == 3 && bin > 0) {
+            const unsigned int over = ((unsigned)bin > d.value ? front[0] : 0u) + ((unsigned)(bin - 1) > d.value ? front[1] : 0u);
+            const unsigned int tie = ((unsigned)bin == d.value ? front[0] : 0u) + ((unsigned)(bin - 1) == d.value ? front[1] : 0u);
+            if (over) atomicAdd(&before[0], over);
+            if (tie) atomicAdd(&before[1], tie);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < kPartR; ++j) key[j] = weight_key(w[j]);
+    if (LEVEL < 3) {
+        count_digits<kPartR>(hist, key, p0, lo, hi, border, LEVEL, tid);
+        unsigned int *out = LEVEL == 2 ? own->last : own->hist[LEVEL & 1];
+        for (int i = tid; i < (LEVEL == 2 ? 1024 : 2048); i += kEvictThreads) out[i] = hist[i];
+        if (LEVEL >= 1) {
+            // keys above the border by the digit that this launch has found (equal in the digits before it)
+            unsigned int n = 0;
+#pragma unroll
+            for (int j = 0; j < kPartR; ++j) {
+                const bool over = LEVEL == 1 ? key[j] >> 21 > border >> 21 : (key[j] >> 21 == border >> 21 && key[j] >> 10 > border >> 10);
+                const int i = p0 + j * kEvictThreads + tid;
+                n += (unsigned)__popcll(__ballot(i >= lo && i < hi && over));
+            }
+            if ((tid & 63) == 0) sh[tid >> 6] = n;
+            __syncthreads();
+            if (tid == 0) {
+                unsigned int t = 0;
+                for (int v = 0; v < kEvictThreads / 64; ++v) t += sh[v];
+                own->above[LEVEL - 1] = t;
+            }
+        }
+        if (LEVEL >= 1 && part == 0 && tid == 0) {
+            // (a place of each launch's own: this one's workgroups read what the one before it left)
+            own->border[LEVEL - 1] = border;
+            own->left[LEVEL - 1] = left;
         }
         return;
     }
-    // of the positions [lo, hi) the `want` largest
-    const int lo = a.n_first, hi = len - a.n_recent, want = a.n_keep - a.n_first - a.n_recent;
-    unsigned int prefix = 0, left = (unsigned)want;
-    for (int shift = 24; shift >= 0 && want > 0; shift -= 8) {
-        if (tid < 256) hist[tid] = 0;
-        __syncthreads();
-        for (int i = lo + tid; i < hi; i += 1024) {
-            const unsigned int k = weight_key(w[i]);
-            if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255u], 1u);
-        }
-        __syncthreads();
-        if (tid == 0) {
-            unsigned int above = 0;
-            int d = 255;
-            while (d > 0 && above + hist[d] < left) above += hist[d--];
-            s_prefix = prefix | (unsigned)d << shift;
-            s_left = left - above;
-        }
-        __syncthreads();
-        prefix = s_prefix;
-        left = s_left;
+    __syncthreads();
+    // positions that stay in front of this part
+    const int outer = min(p0, lo) + max(0, p0 - max(hi, lo));
+    unsigned int at = (unsigned)outer, ties = 0;
+    if (want > 0) {
+#pragma unroll 8
+        for (int c = 0; c < part; ++c) at += seq[c].above[0] + seq[c].above[1];
+        ties = before[1];
+        at += before[0] + min(ties, left);
     }
-    // prefix is the key of the last one taken, `left` of the positions that have it are taken, the lowest
-    int done = 0;
-    unsigned int ties = 0;
-    for (int i0 = 0; i0 < len; i0 += 1024) {
-        const int i = i0 + tid;
-        bool above = false, tie = false;
-        float x = 0.f;
-        if (i < len) {
-            x = w[i];
-            const unsigned int k = weight_key(x);
-            const bool inner = i >= lo && i < hi;
-            above = !inner || (want > 0 && k > prefix);
-            tie = inner && want > 0 && k == prefix;
-        }
-        const unsigned long long mt = __ballot(tie), below = (1ull << lane) - 1;
-        if (lane == 0) wave_n[0][wave] = __popcll(mt);
-        __syncthreads();
-        unsigned int before = ties, all = ties;
-        for (int v = 0; v < 16; ++v) {
-            if (v < wave) before += wave_n[0][v];
-            all += wave_n[0][v];
-        }
-        const bool take = above || (tie && before + __popcll(mt & below) < left);
-        ties = all;
-        const unsigned long long mk = __ballot(take);
-        if (lane == 0) wave_n[1][wave] = __popcll(mk);
-        __syncthreads();
-        int at = done;
-        for (int v = 0; v < 16; ++v) {
-            if (v < wave) at += wave_n[1][v];
-            done += wave_n[1][v];
-        }
-        at += __popcll(mk & below);
-        if (take && at < a.n_keep) {
-            keep[at] = i;
-            if (kept) kept[at] = x;
-        }
-        __syncthreads();
-    }
+    emit_kept<kPartR>(a, b, p0, lo, hi, len, want > 0, border, left, ties, at, key, w, runs, tid);
 }
 
 constexpr int kMoveRows = 32;                 // rows of a workgroup
@@ -225,9 +413,29 @@ hipError_t launch_weight_add(const WeightArgs &a, hipStream_t st)
     return hipGetLastError();
 }
 
-hipError_t launch_evict_keep(const EvictArgs &a, hipStream_t st)
+// A workgroup holds up to 32768 keys; longer sequences are taken in parts.
+int evict_parts(int Lk) { return Lk <= 32 * kEvictThreads ? 0 : (Lk + kPart - 1) / kPart; }
+size_t evict_ws_bytes(int B, int Lk) { return (size_t)B * evict_parts(Lk) * sizeof(PartCounts); }
+
+hipError_t launch_evict_keep(EvictArgs a, hipStream_t st)
 {
-    hipLaunchKernelGGL(evict_kernel, dim3((unsigned)a.B), dim3(1024), 0, st, a);
+    a.n_parts = evict_parts(a.Lk);
+    if (a.n_parts == 0) {
+        const int per = (a.Lk + kEvictThreads - 1) / kEvictThreads;
+        const dim3 grid((unsigned)a.B), block(kEvictThreads);
+        if (per <= 1)
+            hipLaunchKernelGGL((evict_kernel<1>), grid, block, 0, st, a);
+        else if (per <= 8)
+            hipLaunchKernelGGL((evict_kernel<8>), grid, block, 0, st, a);
+        else
+            hipLaunchKernelGGL((evict_kernel<32>), grid, block, 0, st, a);
+        return hipGetLastError();
+    }
+    const dim3 grid((unsigned)(a.B * a.n_parts)), block(kEvictThreads);
+    hipLaunchKernelGGL((evict_part_kernel<0>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((evict_part_kernel<1>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((evict_part_kernel<2>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((evict_part_kernel<3>), grid, block, 0, st, a);
     return hipGetLastError();
 }
 
