@@ -16,6 +16,9 @@
 //   kv4_read_kernel   the way back to bf16, exact.
 //   kv4_attn_kernel   O = softmax(sm_scale Q K^T) V over the rows that idx names.  See there.
 //   kv4_probs_kernel  the heads' mean of that softmax per selected row, from the log-sum-exps.
+#include <algorithm>
+#include <cstddef>
+
 #include "ic_common.hpp"
 
 namespace ic {
@@ -25,6 +28,7 @@ namespace {
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
 typedef __attribute__((ext_vector_type(2))) int i32x2;
+typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(2))) unsigned int u32x2;
 
 constexpr int kRowB = IC_KV4_ROW_BYTES;
@@ -191,6 +195,99 @@ __device__ __forceinline__ void fetch_tile(const unsigned char *kv4, int row, un
     }
 }
 
+// The lane's number, worked out where it is needed: kept, it and what depends on it would take registers from O^T and Q.
+__device__ __forceinline__ int lane_now()
+{
+    int l;
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
+    return l;
+}
+
+// 32 words (lanes 0-31) to LDS, one behind the other.
+__device__ __forceinline__ void fetch_words(const int32_t *p, unsigned int lds, int lane)
+{
+    if (lane < 32) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(p) : "memory");
+}
+
+// What a wave fetches, tile after tile of all of its queries, ahead of what it computes: a step asks for the rows of the tile two
+// steps on, the page numbers of the one four on and the entries of idx of the one six on, 18 instructions that leave nothing
+// in registers.  Loads return in order, so 18 outstanding at the beginning of a step mean that everything from the step
+// before the last has arrived.  (Nothing else loads within the loop over a query's tiles.)
+constexpr int kAhead = 18;
+struct Words {
+    int32_t idx[8][kT], page[4][kT];          // of tile n in [n % 8], [n % 4]
+};
+struct Cursor {
+    int q;                                    // query row; n_queries and more: none
+    int tile, b, len;                         // len: 0 where there is no such tile
+};
+
+template <int W>
+struct Fetch {
+    const Kv4AttnArgs &a;
+    Words *words;
+    unsigned int words0, ring0;               // LDS
+    int nq, stride;                           // (B Tq is below 2^30, a stride 1024 at most)
+    int s0, s1, n_tiles, first;
+    Cursor rows, pages, ids;
+    unsigned int n;                           // tile number of `rows`
+
+    __device__ __forceinline__ Fetch(const Kv4AttnArgs &a_, Words *w, unsigned int ring, int q, int stride_, int split, int first_)
+        : a(a_), words(w), ring0(ring), nq(a_.B * a_.Tq), stride(stride_), first(first_)
+    {
+        words0 = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_offset(w));
+        s0 = split * a.split_len;
+        s1 = min(s0 + a.split_len, a.k_sel);
+        n_tiles = (s1 - s0 + kT - 1) / kT;
+        rows.q = q;
+        rows.tile = first;
+        place(rows);
+        pages = ids = rows;
+        n = 0;
+    }
+    __device__ __forceinline__ void place(Cursor &c) const
+    {
+        const bool there = c.q < nq && c.tile < n_tiles;
+        c.b = there ? (int)((unsigned)c.q / (unsigned)a.Tq) : 0;
+        c.len = there ? (a.pv.seq_lens ? min(load_uniform(a.pv.seq_lens + c.b), a.Lk) : a.Lk) : 0;
+    }
+    __device__ __forceinline__ void next(Cursor &c) const
+    {
+        c.tile += W;
+        if (c.tile >= n_tiles) {
+            c.tile = first;
+            c.q += W == 1 ? stride : nq;      // (waves that share a query have one)
+            place(c);
+        }
+    }
+    __device__ __forceinline__ void ask_ids(unsigned int m, int lane)
+    {
+        const int64_t q = min(ids.q, nq - 1);
+        const int s = min(s0 + ids.tile * kT + (lane & 31), a.k_sel - 1);
+        fetch_words(a.idx + q * a.k_sel + s, words0 + (m & 7) * (kT * 4), lane);
+        next(ids);
+    }
+    __device__ __forceinline__ void ask_pages(unsigned int m, int lane)
+    {
+        const int s = words->idx[m & 7][lane & 31];
+        const int32_t *p = a.idx;             // (not paged: any word)
+        if (a.pv.page_table) p = a.pv.page_table + (int64_t)pages.b * a.pv.max_pages + (s >= 0 && s < pages.len ? s >> a.pv.page_shift : 0);
+        fetch_words(p, words0 + (unsigned)offsetof(Words, page) + (m & 3) * (kT * 4), lane);
+        next(pages);
+    }
+    // the rows of tile m into LDS at `at`; returns which of them there are
+    __device__ __forceinline__ unsigned int ask_rows(unsigned int m, unsigned int at, int lane)
+    {
+        const int s = words->idx[m & 7][lane & 31], page = words->page[m & 3][lane & 31];
+        const int slot = s0 + rows.tile * kT + (lane & 31);
+        int64_t r = a.pv.page_table ? ((int64_t)page << a.pv.page_shift) + (s & ((1 << a.pv.page_shift) - 1)) : (int64_t)rows.b * a.Lk + s;
+        const bool there = slot < s1 && s >= 0 && s < rows.len && r >= 0 && r < a.pool_rows;
+        fetch_tile((const unsigned char *)a.KV4, there ? (int)r : -1, ring0 + at, lane);
+        next(rows);
+        return (unsigned int)__ballot(there);
+    }
+};
+
 __device__ __forceinline__ float half_max(float x) { return fmaxf(x, __shfl_xor(x, 32)); }
 __device__ __forceinline__ float half_sum(float x) { return x + __shfl_xor(x, 32); }
 
@@ -211,38 +308,80 @@ __device__ __forceinline__ void scale_tiles(f32x16 (&o)[16], float f)
     asm volatile("s_nop 7\n\ts_nop 7" ::: "memory");
 }
 
+// Four registers of a tile of O^T, times f: read where they are used (all 256 at once would displace everything else).
+__device__ __forceinline__ f32x4 read4(const f32x16 &o, int i4, float f)
+{
+    f32x4 y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        float x;
+        asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(x) : "a"(o[4 * i4 + e]));
+        y[e] = x * f;
+    }
+    return y;
+}
+
+// Four products into an accumulator that lives in ordinary registers: O^T takes all of the accumulation registers, and left to
+// itself the compiler puts every accumulator there.  It knows nothing of these instructions' timing, so each brings the two
+// wait states behind the conversions that wrote its operands, and the last the wait for its result.
+__device__ __forceinline__ void mfma4_first(f32x16 &s, bf16x8 a0, bf16x8 a1, bf16x8 a2, bf16x8 a3, const bf16x8 (&b)[4])
+{
+    asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %5, 0\n\tv_mfma_f32_32x32x16_bf16 %0, %2, %6, %0\n\t"
+        "v_mfma_f32_32x32x16_bf16 %0, %3, %7, %0\n\tv_mfma_f32_32x32x16_bf16 %0, %4, %8, %0"
+        : "=&v"(s) : "v"(a0), "v"(a1), "v"(a2), "v"(a3), "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]));
+}
+__device__ __forceinline__ void mfma4(f32x16 &s, bf16x8 a0, bf16x8 a1, bf16x8 a2, bf16x8 a3, const bf16x8 (&b)[4])
+{
+    asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %5, %0\n\tv_mfma_f32_32x32x16_bf16 %0, %2, %6, %0\n\t"
+        "v_mfma_f32_32x32x16_bf16 %0, %3, %7, %0\n\tv_mfma_f32_32x32x16_bf16 %0, %4, %8, %0"
+        : "+v"(s) : "v"(a0), "v"(a1), "v"(a2), "v"(a3), "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]));
+}
+__device__ __forceinline__ void mfma4_last(f32x16 &s, bf16x8 a0, bf16x8 a1, bf16x8 a2, bf16x8 a3, const bf16x8 (&b)[4])
+{
+    asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %5, %0\n\tv_mfma_f32_32x32x16_bf16 %0, %2, %6, %0\n\t"
+        "v_mfma_f32_32x32x16_bf16 %0, %3, %7, %0\n\tv_mfma_f32_32x32x16_bf16 %0, %4, %8, %0\n\ts_nop 15\n\ts_nop 7"
+        : "+v"(s) : "v"(a0), "v"(a1), "v"(a2), "v"(a3), "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]));
+}
+
 // W waves of the workgroup share a (query, split): each takes every W-th tile and they meet at the end.
 template <int W>
 __global__ __launch_bounds__(256, 1) void kv4_attn_kernel(Kv4AttnArgs a)
 {
     __shared__ __attribute__((aligned(16))) unsigned char ring[4][kRing][kTileB];
     __shared__ __attribute__((aligned(16))) unsigned short amounts[4][2][4][2][16];   // [wave][turn][block][half][register]
+    __shared__ Words words[4];
     __shared__ float wave_ml[4][2][32];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, g = lane >> 5;
-    const int64_t nq = (int64_t)a.B * a.Tq, units = nq * a.n_splits;
-    const int64_t unit = W == 1 ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x;
-    if (W == 1 && unit >= units) return;
-    const int64_t q = unit / a.n_splits;
-    const int split = (int)(unit - q * a.n_splits);
-    const int b = (int)(q / a.Tq);
-    const int len = seq_len(a.pv, b, a.Lk);
-    const int s0 = split * a.split_len, s1 = min(s0 + a.split_len, a.k_sel);
-    const int32_t *idx = a.idx + q * a.k_sel;
-    const unsigned char *kv4 = (const unsigned char *)a.KV4;
-
-    // Q as the B operand: head l32; chunk j, step s: features 64 j + 32 g + 8 s ..; then the rotary ones, 16 r + 8 g ..
+    const int nq = a.B * a.Tq;
+    // W = 1: the waves of an XCD (every eighth workgroup) walk through neighbouring queries, whose selections overlap
+    const int wg = (int)blockIdx.x, wgs = (int)gridDim.x;
+    const int q0 = W > 1 ? wg / a.n_splits : (wgs & 7) == 0 ? ((wg & 7) * (wgs >> 3) + (wg >> 3)) * 4 + wave : wg * 4 + wave;
+    const int split = W > 1 ? wg - q0 * a.n_splits : 0;
+    if (W == 1 && q0 >= nq) return;
+    Fetch<W> f(a, &words[wave], (unsigned)__builtin_amdgcn_readfirstlane((int)lds_offset(&ring[wave][0][0])), q0, wgs * 4, split, W == 1 ? 0 : wave);
+#pragma unroll
+    for (unsigned int i = 0; i < 6; ++i) f.ask_ids(i, lane);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+    for (unsigned int i = 0; i < 4; ++i) f.ask_pages(i, lane);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    unsigned int ok0 = f.ask_rows(0, 0, lane), ok1 = f.ask_rows(1, kTileB, lane);       // rows that the tiles in the ring have
+    unsigned int n = 0, at = 0, at2 = 2 * kTileB;                           // tile number; in the ring: the tile, the one two behind it
+#pragma unroll 1
+  for (int q = q0; q < nq; q += f.stride) {
+    // Q as the B operand: head l32; chunk j, step s: features 64 j + 32 g + 8 s ..; then the rotary ones, 16 r + 8 g ..  (Lanes
+    // without a head take the first one, and write nothing.)
     bf16x8 ql[8][4], qr[4];
     {
-        const unsigned short *qp = (const unsigned short *)a.Q + (q * a.H_q + (l32 < a.H_q ? l32 : 0)) * kRow;
-        const u32x4 zero = u32x4{0u, 0u, 0u, 0u};
+        const unsigned short *qp = (const unsigned short *)a.Q + ((int64_t)q * a.H_q + (l32 < a.H_q ? l32 : 0)) * kRow;
 #pragma unroll
         for (int j = 0; j < 8; ++j)
 #pragma unroll
             for (int s = 0; s < 4; ++s)
-                ql[j][s] = __builtin_bit_cast(bf16x8, l32 < a.H_q ? *(const u32x4 *)(qp + 64 * j + 32 * g + 8 * s) : zero);
+                ql[j][s] = *(const bf16x8 *)(qp + 64 * j + 32 * g + 8 * s);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) qr[r] = __builtin_bit_cast(bf16x8, l32 < a.H_q ? *(const u32x4 *)(qp + kLat + 16 * r + 8 * g) : zero);
+        for (int r = 0; r < 4; ++r) qr[r] = *(const bf16x8 *)(qp + kLat + 16 * r + 8 * g);
     }
 
     f32x16 o[16];
@@ -252,29 +391,31 @@ __global__ __launch_bounds__(256, 1) void kv4_attn_kernel(Kv4AttnArgs a)
         for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
     float m = -INFINITY, l = 0.f;
 
-    auto row_of = [&](int tile) -> int {
-        const int s = s0 + tile * kT + l32;
-        if (s >= s1) return -1;
-        return (int)kv4_row(a.pv, b, idx[s], len, a.Lk, a.pool_rows);
+    // (Q has arrived before the loop, which must not wait for it, and is in these registers throughout)
+    auto pin = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) asm volatile("" : "+v"(ql[j][0]), "+v"(ql[j][1]), "+v"(ql[j][2]), "+v"(ql[j][3]));
+        asm volatile("" : "+v"(qr[0]), "+v"(qr[1]), "+v"(qr[2]), "+v"(qr[3]));
     };
-    const int n_tiles = (s1 - s0 + kT - 1) / kT, first = W == 1 ? 0 : wave;
-    const unsigned int ring0 = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_offset(&ring[wave][0][0]));
-    int row0 = first < n_tiles ? row_of(first) : -1, row1 = first + W < n_tiles ? row_of(first + W) : -1;   // of the tiles in the ring
-    fetch_tile(kv4, row0, ring0, lane);
-    fetch_tile(kv4, row1, ring0 + kTileB, lane);
-    unsigned int at = 0, at2 = 2 * kTileB;     // in the ring: the tile, the one two behind it
+    pin();
 #pragma unroll 1
-    for (int t = first; t < n_tiles; t += W) {
+    for (int t = f.first; t < f.n_tiles; t += W) {
 #pragma unroll
         for (int t2 = 0; t2 < 16; ++t2) asm volatile("" : "+a"(o[t2]));
+        pin();
         const unsigned char *buf = &ring[wave][0][0] + at;
-        const int row2 = t + 2 * W < n_tiles ? row_of(t + 2 * W) : -1;
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                  // the slot's reads are through
-        fetch_tile(kv4, row2, ring0 + at2, lane);
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * 16) : "memory");       // all but the two newest tiles have arrived
-        const unsigned long long have = __ballot(row0 >= 0);
-        const unsigned int ok = (unsigned int)have;                         // bit: tile row
-
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kAhead) : "memory");   // (and the reads of the ring's free tile are through)
+        const int ln = lane_now(), l32 = ln & 31, g = ln >> 5;
+        const unsigned int ok2 = f.ask_rows(n + 2, at2, ln);
+        f.ask_pages(n + 4, ln);
+        f.ask_ids(n + 6, ln);
+        ++n;
+        const unsigned int ok = ok0;                                        // bit: tile row
+        ok0 = ok1;
+        ok1 = ok2;
+        at = at == 2 * kTileB ? 0 : at + kTileB;
+        at2 = at2 == 2 * kTileB ? 0 : at2 + kTileB;
+        if (ok == 0u) continue;
         // S = K Q^T
         const unsigned char *kp = buf + tile_row(l32) * kRowB;
         const unsigned int sc = *(const unsigned int *)(kp + kScaleOff);
@@ -287,20 +428,22 @@ __global__ __launch_bounds__(256, 1) void kv4_attn_kernel(Kv4AttnArgs a)
             }
         }
         f32x16 s;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+        u32x4 kc[2];                            // (what is read ahead is bounded by hand: the compiler counts on registers that O^T has)
+        kc[0] = *(const u32x4 *)(kp + g * 16);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const u32x4 c = *(const u32x4 *)(kp + (2 * j + g) * 16);
+            if (j < 7) kc[(j + 1) & 1] = *(const u32x4 *)(kp + (2 * (j + 1) + g) * 16);
+            const u32x4 c = kc[j & 1];
             const float f = scale_of((sc >> (8 * (j >> 1))) & 255u);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(c[e], f), ql[j][e], s, 0, 0, 0);
+            if (j == 0)
+                mfma4_first(s, widen(c[0], f), widen(c[1], f), widen(c[2], f), widen(c[3], f), ql[j]);
+            else
+                mfma4(s, widen(c[0], f), widen(c[1], f), widen(c[2], f), widen(c[3], f), ql[j]);
+            __builtin_amdgcn_sched_barrier(0);
         }
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const bf16x8 k = *(const bf16x8 *)(kp + kRopeOff + 32 * r + 16 * g);
-            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, qr[r], s, 0, 0, 0);
-        }
+        mfma4_last(s, *(const bf16x8 *)(kp + kRopeOff + 16 * g), *(const bf16x8 *)(kp + kRopeOff + 32 + 16 * g), *(const bf16x8 *)(kp + kRopeOff + 64 + 16 * g),
+                   *(const bf16x8 *)(kp + kRopeOff + 96 + 16 * g), qr);
+        __builtin_amdgcn_sched_barrier(0);
         // register i is matrix row 8 (i / 4) + 4 g + i % 4
         if (ok != 0xFFFFFFFFu) {
 #pragma unroll
@@ -320,7 +463,7 @@ __global__ __launch_bounds__(256, 1) void kv4_attn_kernel(Kv4AttnArgs a)
             const float mn = fmaxf(m, top), keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
             m = mn;
             l *= keep;
-            if (t != first) scale_tiles(o, keep);
+            scale_tiles(o, keep);
         }
         const float ref = m == -INFINITY ? 0.f : m - kPBias;
         u16x2 p[8];
@@ -328,14 +471,14 @@ __global__ __launch_bounds__(256, 1) void kv4_attn_kernel(Kv4AttnArgs a)
         for (int i = 0; i < 16; i += 2) {
             const float p0 = __builtin_amdgcn_exp2f(s[i] - ref), p1 = __builtin_amdgcn_exp2f(s[i + 1] - ref);
             l += p0 + p1;
-            bf16x2 pk;
-            pk[0] = (__bf16)p0;
-            pk[1] = (__bf16)p1;
-            p[i >> 1] = __builtin_bit_cast(u16x2, pk);
+            p[i >> 1] = __builtin_bit_cast(u16x2, __builtin_convertvector((f32x2{p0, p1}), bf16x2));
         }
         // O^T += V^T P^T
-        const int vm = 8 * ((lane & 15) >> 2) + 4 * g + (lane & 3);
-        const unsigned char *vp = buf + tile_row(vm) * kRowB + ((lane >> 4) & 1) * 8;
+        const int vm = 8 * ((ln & 15) >> 2) + 4 * g + (ln & 3);
+        const unsigned char *vp = buf + tile_row(vm) * kRowB + ((ln >> 4) & 1) * 8;
+        typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
+        i32x2 vc[2];
+        vc[0] = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2 *)vp);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             u32x4 d[2];
@@ -347,24 +490,22 @@ __global__ __launch_bounds__(256, 1) void kv4_attn_kernel(Kv4AttnArgs a)
                 pj[i >> 2][i & 3] = __builtin_bit_cast(unsigned int, __builtin_elementwise_sub_sat(p[i], as_u16x2(d[i >> 2][i & 3])));
 #pragma unroll
             for (int t4 = 0; t4 < 4; ++t4) {
-                typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
-                const i32x2 c = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2 *)(vp + (4 * j + t4) * 16));
-                o[4 * j + t4] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen((unsigned)c[0], 1.f), __builtin_bit_cast(bf16x8, pj[0]), o[4 * j + t4], 0, 0, 0);
-                o[4 * j + t4] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen((unsigned)c[1], 1.f), __builtin_bit_cast(bf16x8, pj[1]), o[4 * j + t4], 0, 0, 0);
+                const int ft = 4 * j + t4;
+                if (ft < 15) vc[(ft + 1) & 1] = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2 *)(vp + (ft + 1) * 16));
+                const i32x2 c = vc[ft & 1];
+                o[ft] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen((unsigned)c[0], 1.f), __builtin_bit_cast(bf16x8, pj[0]), o[ft], 0, 0, 0);
+                o[ft] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen((unsigned)c[1], 1.f), __builtin_bit_cast(bf16x8, pj[1]), o[ft], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
-        row0 = row1;
-        row1 = row2;
-        at = at == 2 * kTileB ? 0 : at + kTileB;
-        at2 = at2 == 2 * kTileB ? 0 : at2 + kTileB;
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 7" ::: "memory");              // (the last products, before their sums are read)
     l = half_sum(l);
 
-    constexpr int kOwn = 16 / W;               // feature tiles whose output this wave writes
-    f32x16 (&r)[16] = o;
+    float mine = 1.f;                          // weight of this wave's part
     if constexpr (W > 1) {
         // the waves' parts: weights by their maxima, then each wave sums a quarter of the features, in two rounds through the rings
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                    // nothing more arrives in the rings
         __syncthreads();
         if (g == 0) {
             wave_ml[wave][0][l32] = m;
@@ -379,11 +520,31 @@ __global__ __launch_bounds__(256, 1) void kv4_attn_kernel(Kv4AttnArgs a)
             const float mw = wave_ml[w][0][l32];
             lt += mw == -INFINITY ? 0.f * wave_ml[w][1][l32] : wave_ml[w][1][l32] * __builtin_amdgcn_exp2f(mw - mt);
         }
-        const float mine = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mt);
+        mine = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mt);
         m = mt;
         l = lt;
+    }
+    const float inv = l == 0.f ? 0.f : 0x1p100f / l;                        // (the sums of P V are without the bias)
+    const bool mine_h = l32 < a.H_q;
+    const int64_t head = (int64_t)q * a.H_q + l32, part = ((int64_t)q * a.n_splits + split) * a.H_q + l32;
+    // features 32 ft + 8 i4 + 4 g + 0 .. 3 of the head
+    auto store = [&](int ft, int i4, f32x4 y) __attribute__((always_inline)) {
+        const int f = 32 * ft + 8 * i4 + 4 * g;
+        if (!mine_h) return;
+        if (W > 1 && a.n_splits > 1) {
+            *(f32x4 *)((float *)a.part_o + part * kLat + f) = y * inv;
+        } else {
+            typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+            *(bf16x4 *)((__bf16 *)a.O + head * kLat + f) = __builtin_convertvector(y * inv, bf16x4);
+        }
+    };
+    if constexpr (W == 1) {
+#pragma unroll
+        for (int ft = 0; ft < 16; ++ft)
+#pragma unroll
+            for (int i4 = 0; i4 < 4; ++i4) store(ft, i4, read4(o[ft], i4, 1.f));
+    } else {
         f32x4 *sh = (f32x4 *)&ring[0][0][0];   // [from][owner][tile of the round][register / 4][lane]
-        // (unrolled over the owner with the wave's own tiles chosen by comparison: registers cannot be indexed)
 #pragma unroll
         for (int round = 0; round < 2; ++round) {
 #pragma unroll
@@ -392,10 +553,7 @@ __global__ __launch_bounds__(256, 1) void kv4_attn_kernel(Kv4AttnArgs a)
 #pragma unroll
                     for (int k = 0; k < 2; ++k)
 #pragma unroll
-                        for (int i4 = 0; i4 < 4; ++i4) {
-                            const f32x16 &x = o[4 * w + 2 * round + k];
-                            sh[(((wave * 4 + w) * 2 + k) * 4 + i4) * 64 + lane] = f32x4{x[4 * i4] * mine, x[4 * i4 + 1] * mine, x[4 * i4 + 2] * mine, x[4 * i4 + 3] * mine};
-                        }
+                        for (int i4 = 0; i4 < 4; ++i4) sh[(((wave * 4 + w) * 2 + k) * 4 + i4) * 64 + lane] = read4(o[4 * w + 2 * round + k], i4, mine);
             __syncthreads();
 #pragma unroll
             for (int w = 0; w < W; ++w)
@@ -404,48 +562,26 @@ __global__ __launch_bounds__(256, 1) void kv4_attn_kernel(Kv4AttnArgs a)
                     for (int k = 0; k < 2; ++k)
 #pragma unroll
                         for (int i4 = 0; i4 < 4; ++i4) {
-                            f32x16 &y = o[4 * w + 2 * round + k];
-                            f32x4 x = f32x4{y[4 * i4] * mine, y[4 * i4 + 1] * mine, y[4 * i4 + 2] * mine, y[4 * i4 + 3] * mine};
+                            f32x4 x = read4(o[4 * w + 2 * round + k], i4, mine);
 #pragma unroll
                             for (int from = 0; from < W; ++from)
                                 if (from != w) x += sh[(((from * 4 + w) * 2 + k) * 4 + i4) * 64 + lane];
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) y[4 * i4 + e] = x[e];
+                            store(4 * w + 2 * round + k, i4, x);
                         }
-            __syncthreads();
+            if (round == 0) __syncthreads();
         }
     }
-    const float inv = l == 0.f ? 0.f : 0x1p100f / l;                        // (the sums of P V are without the bias)
-    if (l32 < a.H_q) {
-        if (a.n_splits > 1) {
-            const int64_t part = (q * a.n_splits + split) * a.H_q + l32;
-            if (g == 0 && (W == 1 || wave == 0)) {
-                a.part_ml[2 * part] = l == 0.f ? -INFINITY : (l != l ? l : m);        // (the merge leaves out what has no maximum)
-                a.part_ml[2 * part + 1] = l * 0x1p-100f;
-            }
-        } else if (g == 0 && (W == 1 || wave == 0) && a.lse) {
-            a.lse[q * a.H_q + l32] = l == 0.f ? -INFINITY : (m + __builtin_log2f(l) - kPBias) * 0.6931471805599453f;
+    if (g == 0 && mine_h && (W == 1 || wave == 0)) {
+        if (W > 1 && a.n_splits > 1) {
+            a.part_ml[2 * part] = l == 0.f ? -INFINITY : (l != l ? l : m);   // (the merge leaves out what has no maximum)
+            a.part_ml[2 * part + 1] = l * 0x1p-100f;
+        } else if (a.lse) {
+            a.lse[head] = l == 0.f ? -INFINITY : (m + __builtin_log2f(l) - kPBias) * 0.6931471805599453f;
         }
-#pragma unroll
-        for (int w = 0; w < W; ++w)
-            if (W == 1 || w == wave)
-#pragma unroll
-                for (int k = 0; k < kOwn; ++k)
-#pragma unroll
-                    for (int i4 = 0; i4 < 4; ++i4) {
-                        const int ft = kOwn * w + k, f = 32 * ft + 8 * i4 + 4 * g;
-                        if (a.n_splits > 1) {
-                            const int64_t at = ((q * a.n_splits + split) * a.H_q + l32) * kLat + f;
-                            *(f32x4 *)((float *)a.part_o + at) = f32x4{r[ft][4 * i4] * inv, r[ft][4 * i4 + 1] * inv, r[ft][4 * i4 + 2] * inv, r[ft][4 * i4 + 3] * inv};
-                        } else {
-                            typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
-                            bf16x4 y;
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) y[e] = (__bf16)(r[ft][4 * i4 + e] * inv);
-                            *(bf16x4 *)((__bf16 *)a.O + (q * a.H_q + l32) * kLat + f) = y;
-                        }
-                    }
     }
+    if (W > 1) break;                          // (one query)
+  }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
 
 // ---- the weight each selected row received --------------------------------------------------------------------------
@@ -468,14 +604,13 @@ __global__ __launch_bounds__(256, 1) void kv4_probs_kernel(Kv4AttnArgs a)
     float off[16];                              // of head 8 (i / 4) + 4 g + i % 4, log2 units
     {
         const unsigned short *qp = (const unsigned short *)a.Q + (q * a.H_q + (l32 < a.H_q ? l32 : 0)) * kRow;
-        const u32x4 zero = u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
         for (int j = 0; j < 8; ++j)
 #pragma unroll
             for (int s = 0; s < 4; ++s)
-                ql[j][s] = __builtin_bit_cast(bf16x8, l32 < a.H_q ? *(const u32x4 *)(qp + 64 * j + 32 * g + 8 * s) : zero);
+                ql[j][s] = *(const bf16x8 *)(qp + 64 * j + 32 * g + 8 * s);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) qr[r] = __builtin_bit_cast(bf16x8, l32 < a.H_q ? *(const u32x4 *)(qp + kLat + 16 * r + 8 * g) : zero);
+        for (int r = 0; r < 4; ++r) qr[r] = *(const bf16x8 *)(qp + kLat + 16 * r + 8 * g);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             const int h = 8 * (i >> 2) + 4 * g + (i & 3);
@@ -558,7 +693,7 @@ hipError_t launch_kv4_attn(const Kv4AttnArgs &a, bool together, hipStream_t st)
     if (together)
         hipLaunchKernelGGL((kv4_attn_kernel<4>), dim3((unsigned)units), dim3(256), 0, st, a);
     else
-        hipLaunchKernelGGL((kv4_attn_kernel<1>), dim3((unsigned)((units + 3) / 4)), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((kv4_attn_kernel<1>), dim3((unsigned)std::min<int64_t>(256, (units + 3) / 4)), dim3(256), 0, st, a);
     return hipGetLastError();
 }
 
