@@ -1740,7 +1740,7 @@ ic_status ic_attn_probs_kv4(const ic_attn_desc *d, const ic_paged_cache *pc, int
     const Kv4Splits sp = kv4_splits(d);
     a.n_splits = sp.n;
     a.split_len = sp.len;
-    hipError_t e = ic::launch_kv4_probs(a, (hipStream_t)stream);
+    hipError_t e = ic::launch_kv4_probs(a, sp.together, (hipStream_t)stream);
     if (e != hipSuccess) return fail(IC_ERR_HIP, "4-bit attention-probability launch failed: %s", hipGetErrorString(e));
     return IC_OK;
 }

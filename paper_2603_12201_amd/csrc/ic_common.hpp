@@ -313,7 +313,7 @@ hipError_t launch_calib(int kind, const void *src, void *dst, const int32_t *idx
 hipError_t launch_kv4_write(const Kv4RowsArgs &a, hipStream_t st);
 hipError_t launch_kv4_read(const Kv4RowsArgs &a, hipStream_t st);
 hipError_t launch_kv4_attn(const Kv4AttnArgs &a, bool together, hipStream_t st);
-hipError_t launch_kv4_probs(const Kv4AttnArgs &a, hipStream_t st);
+hipError_t launch_kv4_probs(const Kv4AttnArgs &a, bool together, hipStream_t st);
 void weight_plan(WeightArgs &a);
 hipError_t launch_weight_add(const WeightArgs &a, hipStream_t st);
 size_t evict_ws_bytes(int B, int Lk);

@@ -51,6 +51,7 @@ __device__ __forceinline__ int seq_len(const PagedView &pv, int b, int Lk)
 
 // (by value: a bit cast of a vector's element takes the vector's first)
 __device__ __forceinline__ bf16x2 as_pair(unsigned int x) { return __builtin_bit_cast(bf16x2, x); }
+__device__ __forceinline__ float as_float(unsigned int x) { return __uint_as_float(x); }
 __device__ __forceinline__ u16x2 as_u16x2(unsigned int x) { return __builtin_bit_cast(u16x2, x); }
 
 // Maximum over the 16 lanes of a row, in every lane of it.
@@ -106,10 +107,8 @@ __global__ __launch_bounds__(256) void kv4_write_kernel(Kv4RowsArgs a)
     }
 }
 
-__device__ __forceinline__ float scale_of(unsigned int byte)                // 2^(byte - 127), 255: NaN
-{
-    return __uint_as_float(byte == 255u ? 0x7FC00000u : byte << 23);
-}
+// 2^(byte - 127); 255 makes an infinity of it, times which every code reads as NaN or infinity
+__device__ __forceinline__ float scale_of(unsigned int byte) { return __uint_as_float(byte << 23); }
 
 // eight codes -> eight bf16
 __device__ __forceinline__ bf16x8 widen(unsigned int c, float scale)
@@ -157,42 +156,39 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4RowsArgs a)
 //       V's block j is multiplied with.  P is bf16 there (as V is exact, the one rounding of the product: relative 2^-9); a
 //       power of two is then a subtraction from its exponent, two rows an instruction.  It saturates at zero, and P is held
 //       times 2^100 (kMaxE) so that the difference is never negative.
-// The rows' bytes go from memory into LDS without passing through registers, three tiles of 12800 bytes per wave: 4-bit tiles
-// are what lets all of this fit (a bf16 tile would be three times as large), and no wave waits for another.
-// Registers: 256 of O^T, 144 of Q and about 100 more: one wave per SIMD.
+// The rows' bytes go from memory into LDS without passing through registers; the codes of four tiles, 8 KB each, and the
+// rotary part of one are what a wave has there: bf16 tiles would be three times as large.  No wave waits for another.
+// Registers: 256 of O^T, 144 of Q and about 100 more: one wave per SIMD, which issues in order, so the 68 matrix instructions
+// of a tile (32 clocks each) have the rest, about 6 vector instructions each, dealt out between them by hand: a step multiplies
+// K of one tile and V of the tile before it, and works out the softmax of the former during the latter.
 
 constexpr int kT = 32;                        // rows of a tile
-constexpr int kTileB = kT * kRowB;            // 12800
-constexpr int kRing = 3;
+constexpr int kCodeB = kT * 256, kRopeB = kT * 128;
+constexpr int kRing = 4;                      // tiles whose codes are in LDS
 constexpr float kPBias = 100.f;               // P is held times 2^100
 constexpr float kLag = 12.f;                  // log2 units a row may exceed its reference before the sums are scaled anew: 2^(100 + 12 + 11)
                                               // (2048 rows) is still a float
 constexpr int kAmount = (127 + 100) << 7;     // what the exponent byte b is subtracted from, as a bf16 exponent: (227 - b) << 7
 
-// Rows m and m + 16 of a tile are 6400 bytes apart, the same LDS bank; the transposing read takes rows 0-3, 8-11, 16-19, 24-27
-// (or the others) together, so the matrix row m >= 16 is the tile's row 16 + ((m - 16) ^ 4): then those are 16 different banks.
+// What a wave has in LDS.  Rows lie 256 (128) bytes apart, so a row's 16-byte pieces are stored in an order of its own, piece c
+// of row r at c ^ (r % 16) (of the rotary part at c ^ (r / 2 % 8)): 16 rows' pieces c then are in 16 different bank groups.
+// The transposing read takes matrix rows 0-3, 8-11, 16-19, 24-27 (or the others) together, so the matrix row m >= 16 is the
+// tile's row 16 + ((m - 16) ^ 4): those too are 16 different r % 16.
+struct Tiles {
+    unsigned char code[4][kRing][kCodeB];     // [wave]
+    unsigned char rope[4][kRopeB];
+    int32_t idx[4][8][kT], page[4][4][kT];    // of tile n in [n % 8], [n % 4]
+    unsigned int scale[4][4][kT];             // the rows' four exponent bytes, tile n in [n % 4]
+    unsigned short amount[4][2][4][2][16];    // what is subtracted from P: tile n in [n % 2][block][half][register of the accumulator]
+    unsigned int code_at[4][4][8];            // where the rows of the tile that is asked for next are: row 4 i + k at [k][i],
+    unsigned int rope_at[4][2][8][4];         // row 8 i + k at [n % 2][k][i]
+    float ml[4][2][32];
+};
 __device__ __forceinline__ int tile_row(int m) { return m ^ ((m & 16) >> 2); }
 
 __device__ __forceinline__ unsigned int lds_offset(const void *p)
 {
     return (unsigned int)(uintptr_t)(const __attribute__((address_space(3))) void *)p;
-}
-
-// All 32 rows of a tile, two per instruction: lanes 0-24 the first, 25-49 the second, 16 bytes each; LDS receives them one
-// behind the other.  row: the cache row of tile row (lane & 31), -1: none (row 0 is fetched and not used).
-__device__ __forceinline__ void fetch_tile(const unsigned char *kv4, int row, unsigned int lds, int lane)
-{
-    const int second = lane >= 25 ? 1 : 0, piece = lane - 25 * second;
-    const int safe = row < 0 ? 0 : row;
-    const unsigned char *base = kv4 + 16 * (piece < 25 ? piece : 0);
-    if (lane < 50) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int r = __builtin_amdgcn_ds_bpermute(4 * (2 * i + second), safe);
-            const unsigned char *p = base + (int64_t)r * kRowB;
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds + i * 2 * kRowB), "v"(p) : "memory");
-        }
-    }
 }
 
 // The lane's number, worked out where it is needed: kept, it and what depends on it would take registers from O^T and Q.
@@ -203,109 +199,220 @@ __device__ __forceinline__ int lane_now()
     return l;
 }
 
-// 32 words (lanes 0-31) to LDS, one behind the other.
-__device__ __forceinline__ void fetch_words(const int32_t *p, unsigned int lds, int lane)
+// 16 bytes per lane, or 4 for lanes 0-31, to LDS at lds + at, one behind the other; from an address of its own, or a base and an
+// offset r + piece.  (All 64 lanes are active where these are called.  m0 is written two instructions ahead of its use.)
+__device__ __forceinline__ void to_lds16(const void *p, unsigned int lds, int at)
 {
-    if (lane < 32) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(p) : "memory");
+    asm volatile("s_add_u32 m0, %0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p), "s"(at) : "memory", "scc");
+}
+__device__ __forceinline__ void to_lds16(const void *base, unsigned int r, unsigned int piece, unsigned int lds, int at)
+{
+    unsigned int off;
+    asm volatile("s_add_u32 m0, %1, %4\n\tv_add_u32 %0, %2, %3\n\tglobal_load_lds_dwordx4 %0, %5" : "=&v"(off) : "s"(lds), "v"(r), "v"(piece), "i"(at), "s"(base) : "memory", "scc");
+}
+__device__ __forceinline__ void to_lds4(const void *p, unsigned int lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_mov_b32 exec_hi, 0\n\tglobal_load_lds_dword %1, off\n\ts_mov_b32 exec_hi, -1" ::"s"(lds), "v"(p) : "memory");
+}
+__device__ __forceinline__ void to_lds4(const void *base, unsigned int off, unsigned int lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_mov_b32 exec_hi, 0\n\tglobal_load_lds_dword %1, %2\n\ts_mov_b32 exec_hi, -1" ::"s"(lds), "v"(off), "s"(base) : "memory");
 }
 
-// What a wave fetches, tile after tile of all of its queries, ahead of what it computes: a step asks for the rows of the tile two
-// steps on, the page numbers of the one four on and the entries of idx of the one six on, 18 instructions that leave nothing
-// in registers.  Loads return in order, so 18 outstanding at the beginning of a step mean that everything from the step
-// before the last has arrived.  (Nothing else loads within the loop over a query's tiles.)
-constexpr int kAhead = 18;
-struct Words {
-    int32_t idx[8][kT], page[4][kT];          // of tile n in [n % 8], [n % 4]
-};
+// What a wave fetches, tile after tile of all of its queries, ahead of what it computes.  In the step of tile n, in this order:
+// the codes of tile n + 2 (8 instructions), the page numbers of n + 4, the entries of idx of n + 6, a wait for all but these 10
+// and the one before them, and when tile n's rotary part has been read that of n + 1 (4) and the exponents of n + 3.  Nothing of
+// it passes through registers, loads return in order, and nothing else loads within the loop over a query's tiles: behind the
+// wait, everything that earlier steps have asked for but their last has arrived.
+constexpr int kAhead = 11;
 struct Cursor {
     int q;                                    // query row; n_queries and more: none
-    int tile, b, len;                         // len: 0 where there is no such tile
+    int tile, b, len;                         // len: 0 where there is no such query
 };
 
-template <int W>
+// W waves share a query: each takes every W-th tile.  WIDE: rows behind 4 GB, in the 32-bit offsets of the others they are not.
+template <int W, bool PAGED, bool WIDE>
 struct Fetch {
     const Kv4AttnArgs &a;
-    Words *words;
-    unsigned int words0, ring0;               // LDS
+    Tiles &lds;
+    unsigned int code0, rope0, idx0, page0, scale0;   // LDS addresses of this wave's
+    int wave;
     int nq, stride;                           // (B Tq is below 2^30, a stride 1024 at most)
-    int s0, s1, n_tiles, first;
+    int s0, n_slots, n_tiles, first;
     Cursor rows, pages, ids;
-    unsigned int n;                           // tile number of `rows`
+    const int32_t *ids_at;                    // idx of the query at `ids`
 
-    __device__ __forceinline__ Fetch(const Kv4AttnArgs &a_, Words *w, unsigned int ring, int q, int stride_, int split, int first_)
-        : a(a_), words(w), ring0(ring), nq(a_.B * a_.Tq), stride(stride_), first(first_)
+    __device__ __forceinline__ Fetch(const Kv4AttnArgs &a_, Tiles &lds_, int wave_, int q, int stride_, int split, int first_)
+        : a(a_), lds(lds_), wave(wave_), nq(a_.B * a_.Tq), stride(stride_), first(first_)
     {
-        words0 = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_offset(w));
+        auto at = [](const void *p) { return (unsigned)__builtin_amdgcn_readfirstlane((int)lds_offset(p)); };
+        code0 = at(&lds.code[wave][0][0]);
+        rope0 = at(&lds.rope[wave][0]);
+        idx0 = at(&lds.idx[wave][0][0]);
+        page0 = at(&lds.page[wave][0][0]);
+        scale0 = at(&lds.scale[wave][0][0]);
         s0 = split * a.split_len;
-        s1 = min(s0 + a.split_len, a.k_sel);
-        n_tiles = (s1 - s0 + kT - 1) / kT;
+        n_slots = min(a.split_len, a.k_sel - s0);
+        n_tiles = (n_slots + kT - 1) / kT;
         rows.q = q;
         rows.tile = first;
         place(rows);
         pages = ids = rows;
-        n = 0;
+        ids_at = a.idx + ((int64_t)min(q, nq - 1) * a.k_sel + s0);
     }
     __device__ __forceinline__ void place(Cursor &c) const
     {
         const bool there = c.q < nq && c.tile < n_tiles;
         c.b = there ? (int)((unsigned)c.q / (unsigned)a.Tq) : 0;
-        c.len = there ? (a.pv.seq_lens ? min(load_uniform(a.pv.seq_lens + c.b), a.Lk) : a.Lk) : 0;
+        c.len = there ? (a.pv.seq_lens ? max(0, min(load_uniform(a.pv.seq_lens + c.b), a.Lk)) : a.Lk) : 0;
     }
-    __device__ __forceinline__ void next(Cursor &c) const
+    __device__ __forceinline__ bool next(Cursor &c) const
     {
         c.tile += W;
-        if (c.tile >= n_tiles) {
-            c.tile = first;
-            c.q += W == 1 ? stride : nq;      // (waves that share a query have one)
-            place(c);
-        }
+        if (c.tile < n_tiles) return false;
+        c.tile = first;
+        c.q += W == 1 ? stride : nq;          // (waves that share a query have one)
+        place(c);
+        return true;
     }
-    __device__ __forceinline__ void ask_ids(unsigned int m, int lane)
+    __device__ __forceinline__ void next_ids()
     {
-        const int64_t q = min(ids.q, nq - 1);
-        const int s = min(s0 + ids.tile * kT + (lane & 31), a.k_sel - 1);
-        fetch_words(a.idx + q * a.k_sel + s, words0 + (m & 7) * (kT * 4), lane);
-        next(ids);
+        if (next(ids)) ids_at = a.idx + ((int64_t)min(ids.q, nq - 1) * a.k_sel + s0);
     }
-    __device__ __forceinline__ void ask_pages(unsigned int m, int lane)
+    __device__ __forceinline__ void advance()
     {
-        const int s = words->idx[m & 7][lane & 31];
-        const int32_t *p = a.idx;             // (not paged: any word)
-        if (a.pv.page_table) p = a.pv.page_table + (int64_t)pages.b * a.pv.max_pages + (s >= 0 && s < pages.len ? s >> a.pv.page_shift : 0);
-        fetch_words(p, words0 + (unsigned)offsetof(Words, page) + (m & 3) * (kT * 4), lane);
-        next(pages);
-    }
-    // the rows of tile m into LDS at `at`; returns which of them there are
-    __device__ __forceinline__ unsigned int ask_rows(unsigned int m, unsigned int at, int lane)
-    {
-        const int s = words->idx[m & 7][lane & 31], page = words->page[m & 3][lane & 31];
-        const int slot = s0 + rows.tile * kT + (lane & 31);
-        int64_t r = a.pv.page_table ? ((int64_t)page << a.pv.page_shift) + (s & ((1 << a.pv.page_shift) - 1)) : (int64_t)rows.b * a.Lk + s;
-        const bool there = slot < s1 && s >= 0 && s < rows.len && r >= 0 && r < a.pool_rows;
-        fetch_tile((const unsigned char *)a.KV4, there ? (int)r : -1, ring0 + at, lane);
         next(rows);
+        next(pages);
+        next_ids();
+    }
+    __device__ __forceinline__ void ask_ids(unsigned int m, int lane) const
+    {
+        const int t = min(ids.tile, n_tiles - 1) * kT;                      // (a wave without a tile asks for the last one)
+        to_lds4(ids_at + t, 4u * min(lane & 31, n_slots - 1 - t), idx0 + (m & 7) * (kT * 4));
+    }
+    __device__ __forceinline__ int entry(unsigned int m, int lane) const { return lds.idx[wave][m & 7][lane & 31]; }
+    __device__ __forceinline__ int page(unsigned int m, int lane) const { return PAGED ? lds.page[wave][m & 3][lane & 31] : 0; }
+    __device__ __forceinline__ void ask_pages(unsigned int m, int s) const        // s: entry() of tile m
+    {
+        if (!PAGED)
+            to_lds4(a.idx, 0u, page0 + (m & 3) * (kT * 4));                 // (any word: the number of loads is the same)
+        else
+            to_lds4(a.pv.page_table + (int64_t)pages.b * a.pv.max_pages, (unsigned)s < (unsigned)pages.len ? 4u * (unsigned)(s >> a.pv.page_shift) : 0u,
+                    page0 + (m & 3) * (kT * 4));
+    }
+    // Finds the rows of the tile m at `rows` (s and pg: its entry() and page()), asks for their exponents and leaves where they are
+    // for ask_code() and ask_rope(): row numbers (WIDE) or byte offsets, of row 0 where there is none.  Returns which there are.
+    __device__ __forceinline__ unsigned int find_rows(unsigned int m, int s, int pg, int lane)
+    {
+        bool there = ((unsigned)s < (unsigned)rows.len) & ((lane & 31) < n_slots - rows.tile * kT);
+        unsigned int r;
+        if (PAGED) {
+            const unsigned int last = (unsigned)(a.pool_rows - 1);
+            r = ((unsigned)pg << a.pv.page_shift) + ((unsigned)s & ((1u << a.pv.page_shift) - 1u));
+            there = there & ((unsigned)pg <= last >> a.pv.page_shift) & (r <= last);
+        } else {
+            r = (unsigned)(rows.b * a.Lk) + (unsigned)s;                    // (B Lk <= pool_rows < 2^31)
+        }
+        r = there ? (WIDE ? r : r * (unsigned)kRowB) : 0u;
+        const int k = lane & 31;
+        lds.code_at[wave][k & 3][k >> 2] = r;                               // (both halves of the lanes write the same)
+        lds.rope_at[wave][m & 1][k & 7][k >> 3] = r;
+        if (WIDE)
+            to_lds4((const unsigned char *)a.KV4 + ((uint64_t)r * kRowB + kScaleOff), scale0 + (m & 3) * (kT * 4));
+        else
+            to_lds4(a.KV4, r + kScaleOff, scale0 + (m & 3) * (kT * 4));
         return (unsigned int)__ballot(there);
+    }
+    template <int AT> __device__ __forceinline__ void ask16(unsigned int r, unsigned int piece, unsigned int to) const
+    {
+        if (WIDE)
+            to_lds16((const unsigned char *)a.KV4 + ((uint64_t)r * kRowB + piece), to, AT);
+        else
+            to_lds16(a.KV4, r, piece, to, AT);
+    }
+    // four rows' codes, 16 lanes each: row 4 i + lane / 16, at code_at[lane / 16][i]
+    __device__ __forceinline__ u32x4 code_rows(int i4, int lane) const { return *(const u32x4 *)&lds.code_at[wave][lane >> 4][4 * i4]; }
+    static __device__ __forceinline__ unsigned int code_piece(int lane) { return 16u * ((lane & 15) ^ (lane >> 4)); }
+    template <int I> __device__ __forceinline__ void ask_code(unsigned int to, unsigned int r, unsigned int piece) const { ask16<I * 1024>(r, piece ^ (64u * (I & 3)), to); }
+    __device__ __forceinline__ unsigned int code_slot(unsigned int m) const { return code0 + (m & (kRing - 1)) * kCodeB; }
+    // eight rows' rotary parts, 8 lanes each: row 8 i + lane / 8
+    __device__ __forceinline__ u32x4 rope_rows(unsigned int m, int lane) const { return *(const u32x4 *)&lds.rope_at[wave][m & 1][lane >> 3][0]; }
+    static __device__ __forceinline__ unsigned int rope_piece(int lane) { return kRopeOff + 16u * ((lane & 7) ^ (lane >> 4)); }
+    template <int I> __device__ __forceinline__ void ask_rope(unsigned int r, unsigned int piece) const { ask16<I * 1024>(r, piece ^ (64u * (I & 1)), rope0); }
+    __device__ __forceinline__ void ask_codes(unsigned int m, int lane) const
+    {
+        const u32x4 r0 = code_rows(0, lane), r1 = code_rows(1, lane);
+        const unsigned int to = code_slot(m), piece = code_piece(lane);
+        ask_code<0>(to, r0[0], piece);
+        ask_code<1>(to, r0[1], piece);
+        ask_code<2>(to, r0[2], piece);
+        ask_code<3>(to, r0[3], piece);
+        ask_code<4>(to, r1[0], piece);
+        ask_code<5>(to, r1[1], piece);
+        ask_code<6>(to, r1[2], piece);
+        ask_code<7>(to, r1[3], piece);
+    }
+    __device__ __forceinline__ void ask_ropes(unsigned int m, int lane) const
+    {
+        const u32x4 r = rope_rows(m, lane);
+        const unsigned int piece = rope_piece(lane);
+        ask_rope<0>(r[0], piece);
+        ask_rope<1>(r[1], piece);
+        ask_rope<2>(r[2], piece);
+        ask_rope<3>(r[3], piece);
+    }
+    // the start: everything that the steps before tile 0's would have asked for
+    __device__ __forceinline__ void begin(int lane, unsigned int (&ok)[3])
+    {
+#pragma unroll 1
+        for (unsigned int i = 0; i < 6; ++i) {
+            ask_ids(i, lane);
+            next_ids();
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll 1
+        for (unsigned int i = 0; i < 4; ++i) {
+            ask_pages(i, entry(i, lane));
+            next(pages);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+        for (unsigned int i = 0; i < 3; ++i) {
+            ok[i] = find_rows(i, entry(i, lane), page(i, lane), lane);
+            next(rows);
+            if (i < 2) ask_codes(i, lane);
+            if (i == 0) ask_ropes(0, lane);
+        }
+        asm volatile("s_waitcnt vmcnt(10)" ::: "memory");                   // (tile 0 has arrived)
     }
 };
 
-__device__ __forceinline__ float half_max(float x) { return fmaxf(x, __shfl_xor(x, 32)); }
-__device__ __forceinline__ float half_sum(float x) { return x + __shfl_xor(x, 32); }
+// Over the lanes l and l + 32.
+__device__ __forceinline__ float half_max(float x)
+{
+    const u32x2 y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(as_float(y[0]), as_float(y[1]));
+}
+__device__ __forceinline__ float half_sum(float x)
+{
+    const u32x2 y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return as_float(y[0]) + as_float(y[1]);
+}
 
-// O^T times a factor per head.  The accumulators live in registers that only matrix instructions and moves reach, and the asm
-// that reads them brings its own wait for the matrix instruction before it.
+// O^T times a factor per head, a tile at a time: the accumulators live in registers that only matrix instructions and moves
+// reach, and all of them out at once would displace everything else.
 __device__ __forceinline__ void scale_tiles(f32x16 (&o)[16], float f)
 {
-    asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 7" ::: "memory");
 #pragma unroll
-    for (int t = 0; t < 16; ++t)
+    for (int t = 0; t < 16; ++t) {
+        f32x16 y = o[t];
+        asm volatile("" : "+v"(y));
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            float x;
-            asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(x) : "a"(o[t][i]));
-            x *= f;
-            asm volatile("v_accvgpr_write_b32 %0, %1" : "=a"(o[t][i]) : "v"(x));
-        }
-    asm volatile("s_nop 7\n\ts_nop 7" ::: "memory");
+        for (int i = 0; i < 16; ++i) y[i] *= f;
+        asm volatile("" : "+a"(y));
+        o[t] = y;
+        __builtin_amdgcn_sched_barrier(0);
+    }
 }
 
 // Four registers of a tile of O^T, times f: read where they are used (all 256 at once would displace everything else).
@@ -321,59 +428,36 @@ __device__ __forceinline__ f32x4 read4(const f32x16 &o, int i4, float f)
     return y;
 }
 
-// Four products into an accumulator that lives in ordinary registers: O^T takes all of the accumulation registers, and left to
-// itself the compiler puts every accumulator there.  It knows nothing of these instructions' timing, so each brings the two
-// wait states behind the conversions that wrote its operands, and the last the wait for its result.
-__device__ __forceinline__ void mfma4_first(f32x16 &s, bf16x8 a0, bf16x8 a1, bf16x8 a2, bf16x8 a3, const bf16x8 (&b)[4])
-{
-    asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %5, 0\n\tv_mfma_f32_32x32x16_bf16 %0, %2, %6, %0\n\t"
-        "v_mfma_f32_32x32x16_bf16 %0, %3, %7, %0\n\tv_mfma_f32_32x32x16_bf16 %0, %4, %8, %0"
-        : "=&v"(s) : "v"(a0), "v"(a1), "v"(a2), "v"(a3), "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]));
-}
-__device__ __forceinline__ void mfma4(f32x16 &s, bf16x8 a0, bf16x8 a1, bf16x8 a2, bf16x8 a3, const bf16x8 (&b)[4])
-{
-    asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %5, %0\n\tv_mfma_f32_32x32x16_bf16 %0, %2, %6, %0\n\t"
-        "v_mfma_f32_32x32x16_bf16 %0, %3, %7, %0\n\tv_mfma_f32_32x32x16_bf16 %0, %4, %8, %0"
-        : "+v"(s) : "v"(a0), "v"(a1), "v"(a2), "v"(a3), "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]));
-}
-__device__ __forceinline__ void mfma4_last(f32x16 &s, bf16x8 a0, bf16x8 a1, bf16x8 a2, bf16x8 a3, const bf16x8 (&b)[4])
-{
-    asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %5, %0\n\tv_mfma_f32_32x32x16_bf16 %0, %2, %6, %0\n\t"
-        "v_mfma_f32_32x32x16_bf16 %0, %3, %7, %0\n\tv_mfma_f32_32x32x16_bf16 %0, %4, %8, %0\n\ts_nop 15\n\ts_nop 7"
-        : "+v"(s) : "v"(a0), "v"(a1), "v"(a2), "v"(a3), "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]));
-}
+// A product into an accumulator that lives in ordinary registers: O^T takes all of the accumulation registers, and left to
+// itself the compiler puts every accumulator there.  It knows nothing of these instructions' timing: between the conversions that
+// write an operand and the product that reads it there is another product (two wait states are needed), and behind the last
+// product comes mfma_settle() (11 wait states before the sum may be read).
+__device__ __forceinline__ void mfma_new(f32x16 &s, bf16x8 x, bf16x8 y) { asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(x), "v"(y)); }
+__device__ __forceinline__ void mfma_add(f32x16 &s, bf16x8 x, bf16x8 y) { asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(x), "v"(y)); }
+__device__ __forceinline__ void mfma_settle(f32x16 &s) { asm volatile("s_nop 13" : "+v"(s)); }
 
 // W waves of the workgroup share a (query, split): each takes every W-th tile and they meet at the end.
-template <int W>
+template <int W, bool PAGED, bool WIDE>
 __global__ __launch_bounds__(256, 1) void kv4_attn_kernel(Kv4AttnArgs a)
 {
-    __shared__ __attribute__((aligned(16))) unsigned char ring[4][kRing][kTileB];
-    __shared__ __attribute__((aligned(16))) unsigned short amounts[4][2][4][2][16];   // [wave][turn][block][half][register]
-    __shared__ Words words[4];
-    __shared__ float wave_ml[4][2][32];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int l32 = lane & 31, g = lane >> 5;
+    __shared__ __attribute__((aligned(1024))) Tiles lds;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int nq = a.B * a.Tq;
     // W = 1: the waves of an XCD (every eighth workgroup) walk through neighbouring queries, whose selections overlap
     const int wg = (int)blockIdx.x, wgs = (int)gridDim.x;
     const int q0 = W > 1 ? wg / a.n_splits : (wgs & 7) == 0 ? ((wg & 7) * (wgs >> 3) + (wg >> 3)) * 4 + wave : wg * 4 + wave;
     const int split = W > 1 ? wg - q0 * a.n_splits : 0;
     if (W == 1 && q0 >= nq) return;
-    Fetch<W> f(a, &words[wave], (unsigned)__builtin_amdgcn_readfirstlane((int)lds_offset(&ring[wave][0][0])), q0, wgs * 4, split, W == 1 ? 0 : wave);
-#pragma unroll
-    for (unsigned int i = 0; i < 6; ++i) f.ask_ids(i, lane);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-#pragma unroll
-    for (unsigned int i = 0; i < 4; ++i) f.ask_pages(i, lane);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    unsigned int ok0 = f.ask_rows(0, 0, lane), ok1 = f.ask_rows(1, kTileB, lane);       // rows that the tiles in the ring have
-    unsigned int n = 0, at = 0, at2 = 2 * kTileB;                           // tile number; in the ring: the tile, the one two behind it
+    Fetch<W, PAGED, WIDE> f(a, lds, wave, q0, wgs * 4, split, W == 1 ? 0 : wave);
+    unsigned int n = 0, ok[3];                 // tile number; which rows it and the next two have
+    f.begin(lane_now(), ok);
 #pragma unroll 1
   for (int q = q0; q < nq; q += f.stride) {
     // Q as the B operand: head l32; chunk j, step s: features 64 j + 32 g + 8 s ..; then the rotary ones, 16 r + 8 g ..  (Lanes
     // without a head take the first one, and write nothing.)
     bf16x8 ql[8][4], qr[4];
     {
+        const int ln = lane_now(), l32 = ln & 31, g = ln >> 5;
         const unsigned short *qp = (const unsigned short *)a.Q + ((int64_t)q * a.H_q + (l32 < a.H_q ? l32 : 0)) * kRow;
 #pragma unroll
         for (int j = 0; j < 8; ++j)
@@ -390,6 +474,9 @@ __global__ __launch_bounds__(256, 1) void kv4_attn_kernel(Kv4AttnArgs a)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
     float m = -INFINITY, l = 0.f;
+    u16x2 p[8];                                // of the tile before: bf16, two rows of the accumulator's registers each
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p[i] = u16x2{0, 0};
 
     // (Q has arrived before the loop, which must not wait for it, and is in these registers throughout)
     auto pin = [&]() __attribute__((always_inline)) {
@@ -398,108 +485,223 @@ __global__ __launch_bounds__(256, 1) void kv4_attn_kernel(Kv4AttnArgs a)
         asm volatile("" : "+v"(qr[0]), "+v"(qr[1]), "+v"(qr[2]), "+v"(qr[3]));
     };
     pin();
-#pragma unroll 1
-    for (int t = f.first; t < f.n_tiles; t += W) {
-#pragma unroll
-        for (int t2 = 0; t2 < 16; ++t2) asm volatile("" : "+a"(o[t2]));
-        pin();
-        const unsigned char *buf = &ring[wave][0][0] + at;
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kAhead) : "memory");   // (and the reads of the ring's free tile are through)
-        const int ln = lane_now(), l32 = ln & 31, g = ln >> 5;
-        const unsigned int ok2 = f.ask_rows(n + 2, at2, ln);
-        f.ask_pages(n + 4, ln);
-        f.ask_ids(n + 6, ln);
-        ++n;
-        const unsigned int ok = ok0;                                        // bit: tile row
-        ok0 = ok1;
-        ok1 = ok2;
-        at = at == 2 * kTileB ? 0 : at + kTileB;
-        at2 = at2 == 2 * kTileB ? 0 : at2 + kTileB;
-        if (ok == 0u) continue;
-        // S = K Q^T
-        const unsigned char *kp = buf + tile_row(l32) * kRowB;
-        const unsigned int sc = *(const unsigned int *)(kp + kScaleOff);
-        {                                       // the subtractions of P's exponents, in the order of the accumulator's registers
-            const int reg = 4 * (l32 >> 3) + (l32 & 3), half = (l32 >> 2) & 1;
-            if (g == 0) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    amounts[wave][0][j][half][reg] = (unsigned short)(kAmount - (int)(((sc >> (8 * j)) & 255u) << 7));
-            }
-        }
-        f32x16 s;
-        u32x4 kc[2];                            // (what is read ahead is bounded by hand: the compiler counts on registers that O^T has)
-        kc[0] = *(const u32x4 *)(kp + g * 16);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            if (j < 7) kc[(j + 1) & 1] = *(const u32x4 *)(kp + (2 * (j + 1) + g) * 16);
-            const u32x4 c = kc[j & 1];
-            const float f = scale_of((sc >> (8 * (j >> 1))) & 255u);
-            if (j == 0)
-                mfma4_first(s, widen(c[0], f), widen(c[1], f), widen(c[2], f), widen(c[3], f), ql[j]);
-            else
-                mfma4(s, widen(c[0], f), widen(c[1], f), widen(c[2], f), widen(c[3], f), ql[j]);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        mfma4_last(s, *(const bf16x8 *)(kp + kRopeOff + 16 * g), *(const bf16x8 *)(kp + kRopeOff + 32 + 16 * g), *(const bf16x8 *)(kp + kRopeOff + 64 + 16 * g),
-                   *(const bf16x8 *)(kp + kRopeOff + 96 + 16 * g), qr);
-        __builtin_amdgcn_sched_barrier(0);
-        // register i is matrix row 8 (i / 4) + 4 g + i % 4
-        if (ok != 0xFFFFFFFFu) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int tr = 8 * (i >> 2) + 4 * (i < 8 ? g : 1 - g) + (i & 3);
-                s[i] = (ok >> tr) & 1u ? s[i] * a.scale_log2e : -INFINITY;
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] *= a.scale_log2e;
-        }
-        float top = s[0];
-#pragma unroll
-        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
-        top = half_max(top);
-        if (__ballot(top > m + kLag) != 0ull) {                             // (m = -inf: the first rows)
-            const float mn = fmaxf(m, top), keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
-            m = mn;
-            l *= keep;
-            scale_tiles(o, keep);
-        }
-        const float ref = m == -INFINITY ? 0.f : m - kPBias;
-        u16x2 p[8];
-#pragma unroll
-        for (int i = 0; i < 16; i += 2) {
-            const float p0 = __builtin_amdgcn_exp2f(s[i] - ref), p1 = __builtin_amdgcn_exp2f(s[i + 1] - ref);
-            l += p0 + p1;
-            p[i >> 1] = __builtin_bit_cast(u16x2, __builtin_convertvector((f32x2{p0, p1}), bf16x2));
-        }
-        // O^T += V^T P^T
-        const int vm = 8 * ((ln & 15) >> 2) + 4 * g + (ln & 3);
-        const unsigned char *vp = buf + tile_row(vm) * kRowB + ((ln >> 4) & 1) * 8;
-        typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
-        i32x2 vc[2];
-        vc[0] = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2 *)vp);
+    typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
+    // V's codes, feature tile ft, as the A operand: lane (feature ln & 31, half g), rows of the accumulator's registers
+    auto v_row = [&](int ln) __attribute__((always_inline)) { return tile_row(8 * ((ln & 15) >> 2) + 4 * (ln >> 5) + (ln & 3)); };
+    auto v_codes = [&](const unsigned char *row, int ft, int r16) __attribute__((always_inline)) -> i32x2 {
+        return __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2 *)(row + ((16 * ft) ^ r16)));
+    };
+    auto v_at = [&](unsigned int m2, int r, int ln) __attribute__((always_inline)) {
+        return &lds.code[wave][0][0] + (m2 & (kRing - 1)) * kCodeB + r * 256 + ((ln >> 4) & 1) * 8;
+    };
+    struct Amount { u32x4 d[2]; };
+    auto amounts = [&](unsigned int m2, int j, int g2) __attribute__((always_inline)) {
+        Amount x;
+        x.d[0] = *(const u32x4 *)&lds.amount[wave][m2 & 1][j][g2][0];
+        x.d[1] = *(const u32x4 *)&lds.amount[wave][m2 & 1][j][g2][8];
+        return x;
+    };
+    auto scaled = [&](u16x2 x, const Amount &am, int i) __attribute__((always_inline)) {
+        return __builtin_bit_cast(unsigned int, __builtin_elementwise_sub_sat(x, as_u16x2(am.d[i >> 2][i & 3])));
+    };
+    // O^T += V^T P^T of the tile before, by itself
+    auto pv_alone = [&](unsigned int m2) __attribute__((always_inline)) {
+        const int ln = lane_now(), r = v_row(ln);
+        const unsigned char *row = v_at(m2, r, ln);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            u32x4 d[2];
-            d[0] = *(const u32x4 *)&amounts[wave][0][j][g][0];
-            d[1] = *(const u32x4 *)&amounts[wave][0][j][g][8];
+            const Amount am = amounts(m2, j, ln >> 5);
             u32x4 pj[2];
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                pj[i >> 2][i & 3] = __builtin_bit_cast(unsigned int, __builtin_elementwise_sub_sat(p[i], as_u16x2(d[i >> 2][i & 3])));
+            for (int i = 0; i < 8; ++i) pj[i >> 2][i & 3] = scaled(p[i], am, i);
 #pragma unroll
             for (int t4 = 0; t4 < 4; ++t4) {
                 const int ft = 4 * j + t4;
-                if (ft < 15) vc[(ft + 1) & 1] = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2 *)(vp + (ft + 1) * 16));
-                const i32x2 c = vc[ft & 1];
+                const i32x2 c = v_codes(row, ft, 16 * (r & 15));
                 o[ft] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen((unsigned)c[0], 1.f), __builtin_bit_cast(bf16x8, pj[0]), o[ft], 0, 0, 0);
                 o[ft] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen((unsigned)c[1], 1.f), __builtin_bit_cast(bf16x8, pj[1]), o[ft], 0, 0, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    bool anew = false;                         // the sums are still by the reference before the last
+    float keep = 1.f;
+    // K's codes, chunk j, as the A operand: lane (row ln & 31, half g)
+    auto k_at = [&](unsigned int m2, int kr) __attribute__((always_inline)) { return &lds.code[wave][0][0] + (m2 & (kRing - 1)) * kCodeB + kr * 256; };
+    auto k_codes = [&](const unsigned char *row, int j, int gr) __attribute__((always_inline)) { return *(const u32x4 *)(row + ((32 * j) ^ gr)); };
+    u32x4 kc[3];                               // chunks j in [j % 3]; of the tile that comes 0 and 1, and its exponents
+    unsigned int sc;
+    {
+        const int ln = lane_now(), kr = tile_row(ln & 31), gr = 16 * ((ln >> 5) ^ (kr & 15));
+        kc[0] = k_codes(k_at(n, kr), 0, gr);
+        kc[1] = k_codes(k_at(n, kr), 1, gr);
+        sc = lds.scale[wave][n & 3][kr];
+    }
+#pragma unroll 1
+    for (int t = f.first; t < f.n_tiles; t += W, ++n) {
+        if (anew) scale_tiles(o, keep);
+#pragma unroll
+        for (int t2 = 0; t2 < 16; ++t2) asm volatile("" : "+a"(o[t2]));
+        pin();
+        const int ln = lane_now(), l32 = ln & 31, g = ln >> 5, kr = tile_row(l32), gr = 16 * (g ^ (kr & 15));
+        f32x16 s;
+        u32x4 pj[2][2];
+        i32x2 vc[4];                            // feature tiles ft in [ft % 4]
+        Amount am;
+        const int vr = v_row(ln), r16 = 16 * (vr & 15);
+        const unsigned int m1 = n - 1;
+        const unsigned char *const vrow = v_at(m1, vr, ln);
+        if (ok[0] == 0u) {
+            // no rows: nothing to score; the tile before may wait for its product
+            f.ask_codes(n + 2, ln);
+            f.ask_pages(n + 4, f.entry(n + 4, ln));
+            f.ask_ids(n + 6, ln);
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kAhead) : "memory");
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = -INFINITY;
+            am = amounts(m1, 0, g);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) pj[0][i >> 2][i & 3] = scaled(p[i], am, i);
+#pragma unroll
+            for (int ft = 0; ft < 3; ++ft) vc[ft] = v_codes(vrow, ft, r16);
+            am = amounts(m1, 1, g);
+        } else {
+            // S = K Q^T of this tile
+            const unsigned char *const krow = k_at(n, kr), *const rrow = &lds.rope[wave][0] + kr * 128;
+            const int rr = 16 * (g ^ (kr >> 1 & 7));
+            auto rope_piece = [&](int r) __attribute__((always_inline)) { return *(const bf16x8 *)(rrow + ((32 * r) ^ rr)); };
+            bf16x8 kb[3], rk[3];
+            u32x4 cr;
+            const unsigned int to = f.code_slot(n + 2), piece = f.code_piece(ln);
+            float sf[4];
+            int pe = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sf[j] = scale_of((sc >> (8 * j)) & 255u);
+            kb[0] = widen(kc[0][0], sf[0]);
+            kb[1] = widen(kc[0][1], sf[0]);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                const int j = i >> 2, e = i & 3;
+                if (i == 0)
+                    mfma_new(s, kb[0], ql[0][0]);
+                else
+                    mfma_add(s, kb[i % 3], ql[j][e]);
+                __builtin_amdgcn_sched_barrier(0);
+                if (i < 30) kb[(i + 2) % 3] = widen(kc[((i + 2) >> 2) % 3][(i + 2) & 3], sf[(i + 2) >> 3]);
+                if (e == 0 && j < 6) kc[(j + 2) % 3] = k_codes(krow, j + 2, gr);
+                if (i == 1 || i == 11) cr = f.code_rows(i > 1, ln);
+                if (i == 6) f.template ask_code<0>(to, cr[0], piece);
+                if (i == 7) f.template ask_code<1>(to, cr[1], piece);
+                if (i == 8) f.template ask_code<2>(to, cr[2], piece);
+                if (i == 9) f.template ask_code<3>(to, cr[3], piece);
+                if (i == 16) f.template ask_code<4>(to, cr[0], piece);
+                if (i == 17) f.template ask_code<5>(to, cr[1], piece);
+                if (i == 18) f.template ask_code<6>(to, cr[2], piece);
+                if (i == 19) f.template ask_code<7>(to, cr[3], piece);
+                if (i == 2 || i == 3 || i == 4 || i == 5) {
+                    // the subtractions from P's exponents, in the order of the accumulator's registers (both halves write the same)
+                    const int jj = i - 2;
+                    lds.amount[wave][n & 1][jj][(l32 >> 2) & 1][4 * (l32 >> 3) + (l32 & 3)] = (unsigned short)(kAmount - (int)(((sc >> (8 * jj)) & 255u) << 7));
+                }
+                if (PAGED && i == 13) pe = f.entry(n + 4, ln);
+                if (i == 20) f.ask_pages(n + 4, pe);
+                if (i == 21) f.ask_ids(n + 6, ln);
+                if (i == 22) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kAhead) : "memory");
+                if (i == 12) am = amounts(m1, 0, g);
+                if (i >= 23 && i < 26) rk[i - 23] = rope_piece(i - 23);
+                if (i >= 26 && i < 30) {
+                    pj[0][(2 * (i - 26)) >> 2][(2 * (i - 26)) & 3] = scaled(p[2 * (i - 26)], am, 2 * (i - 26));
+                    pj[0][(2 * (i - 26) + 1) >> 2][(2 * (i - 26) + 1) & 3] = scaled(p[2 * (i - 26) + 1], am, 2 * (i - 26) + 1);
+                }
+                if (i >= 27 && i < 30) vc[i - 27] = v_codes(vrow, i - 27, r16);
+                if (i == 30) am = amounts(m1, 1, g);
                 __builtin_amdgcn_sched_barrier(0);
             }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                mfma_add(s, rk[r % 3], qr[r]);
+                __builtin_amdgcn_sched_barrier(0);
+                if (r == 0) rk[0] = rope_piece(3);
+            }
+            mfma_settle(s);
+            // register i is matrix row 8 (i / 4) + 4 g + i % 4
+            if (ok[0] != 0xFFFFFFFFu) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int tr = 8 * (i >> 2) + 4 * (i < 8 ? g : 1 - g) + (i & 3);
+                    s[i] = (ok[0] >> tr) & 1u ? s[i] : -INFINITY;
+                }
+            }
         }
+        // O^T += V^T P^T of the tile before, and this tile's P
+        bf16x8 vb[3];
+        unsigned int ok3 = 0;
+        int e3 = 0, p3 = 0;
+        vb[0] = widen((unsigned)vc[0][0], 1.f);
+        vb[1] = widen((unsigned)vc[0][1], 1.f);
+        const u32x4 ro = f.rope_rows(n + 1, ln);
+        const unsigned int rpiece = f.rope_piece(ln);
+        float top = 0.f, ref = 0.f;
+        u16x2 pn[8];
+        float p0 = 0.f;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            const int ft = i >> 1, j = i >> 3, k = i & 7;
+            o[ft] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vb[i % 3], __builtin_bit_cast(bf16x8, pj[j & 1][i & 1]), o[ft], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            if (i < 30) vb[(i + 2) % 3] = widen((unsigned)vc[((i + 2) >> 1) & 3][i & 1], 1.f);
+            if ((i & 1) == 0 && ft + 3 < 16) vc[(ft + 3) & 3] = v_codes(vrow, ft + 3, r16);
+            if (j < 3 && k >= 3 && k < 7) {
+                pj[(j + 1) & 1][(2 * (k - 3)) >> 2][(2 * (k - 3)) & 3] = scaled(p[2 * (k - 3)], am, 2 * (k - 3));
+                pj[(j + 1) & 1][(2 * (k - 3) + 1) >> 2][(2 * (k - 3) + 1) & 3] = scaled(p[2 * (k - 3) + 1], am, 2 * (k - 3) + 1);
+            }
+            if (k == 7 && j < 2) am = amounts(m1, j + 2, g);
+            if (i == 2) top = fmaxf(s[0], s[1]);
+            if (i >= 2 && i < 9) top = fmaxf(fmaxf(top, s[2 * i - 2]), s[2 * i - 1]);
+            if (i == 4) f.template ask_rope<0>(ro[0], rpiece);
+            if (i == 5) f.template ask_rope<1>(ro[1], rpiece);
+            if (i == 6) f.template ask_rope<2>(ro[2], rpiece);
+            if (i == 7) f.template ask_rope<3>(ro[3], rpiece);
+            if (i == 9) {
+                top = half_max(top) * a.scale_log2e;
+                anew = __ballot(top > m + kLag) != 0ull;                    // (m = -inf: the first rows)
+            }
+            if (i == 10) {
+                const float mn = anew ? fmaxf(m, top) : m;
+                keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+                m = mn;
+                l *= keep;
+                ref = m == -INFINITY ? 0.f : m - kPBias;
+            }
+            if (i >= 12 && i < 28) {
+                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i - 12], a.scale_log2e, -ref));
+                l += x;
+                if (i & 1)
+                    pn[(i - 12) >> 1] = __builtin_bit_cast(u16x2, __builtin_convertvector((f32x2{p0, x}), bf16x2));
+                else
+                    p0 = x;
+            }
+            if (i == 8) {
+                e3 = f.entry(n + 3, ln);
+                p3 = f.page(n + 3, ln);
+            }
+            if (i == 16) ok3 = f.find_rows(n + 3, e3, p3, ln);
+            if (i == 22) sc = lds.scale[wave][(n + 1) & 3][kr];
+            if (i == 24) kc[0] = k_codes(k_at(n + 1, kr), 0, gr);
+            if (i == 25) kc[1] = k_codes(k_at(n + 1, kr), 1, gr);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        f.advance();
+        ok[0] = ok[1];
+        ok[1] = ok[2];
+        ok[2] = ok3;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = pn[i];
     }
+    if (anew) scale_tiles(o, keep);
+    pv_alone(n - 1);
     asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 7" ::: "memory");              // (the last products, before their sums are read)
+    const int lane = lane_now(), l32 = lane & 31, g = lane >> 5;
     l = half_sum(l);
 
     float mine = 1.f;                          // weight of this wave's part
@@ -508,17 +710,17 @@ __global__ __launch_bounds__(256, 1) void kv4_attn_kernel(Kv4AttnArgs a)
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                    // nothing more arrives in the rings
         __syncthreads();
         if (g == 0) {
-            wave_ml[wave][0][l32] = m;
-            wave_ml[wave][1][l32] = l;
+            lds.ml[wave][0][l32] = m;
+            lds.ml[wave][1][l32] = l;
         }
         __syncthreads();
         float mt = -INFINITY, lt = 0.f;
 #pragma unroll
-        for (int w = 0; w < W; ++w) mt = fmaxf(mt, wave_ml[w][0][l32]);
+        for (int w = 0; w < W; ++w) mt = fmaxf(mt, lds.ml[w][0][l32]);
 #pragma unroll
         for (int w = 0; w < W; ++w) {
-            const float mw = wave_ml[w][0][l32];
-            lt += mw == -INFINITY ? 0.f * wave_ml[w][1][l32] : wave_ml[w][1][l32] * __builtin_amdgcn_exp2f(mw - mt);
+            const float mw = lds.ml[w][0][l32];
+            lt += mw == -INFINITY ? 0.f * lds.ml[w][1][l32] : lds.ml[w][1][l32] * __builtin_amdgcn_exp2f(mw - mt);
         }
         mine = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mt);
         m = mt;
@@ -544,7 +746,7 @@ __global__ __launch_bounds__(256, 1) void kv4_attn_kernel(Kv4AttnArgs a)
 #pragma unroll
             for (int i4 = 0; i4 < 4; ++i4) store(ft, i4, read4(o[ft], i4, 1.f));
     } else {
-        f32x4 *sh = (f32x4 *)&ring[0][0][0];   // [from][owner][tile of the round][register / 4][lane]
+        f32x4 *sh = (f32x4 *)&lds.code[0][0][0];   // [from][owner][tile of the round][register / 4][lane]
 #pragma unroll
         for (int round = 0; round < 2; ++round) {
 #pragma unroll
@@ -588,22 +790,27 @@ __global__ __launch_bounds__(256, 1) void kv4_attn_kernel(Kv4AttnArgs a)
 //
 // probs[q, slot] = 1/H sum_h exp(sm_scale <Q[h], K[row]> - lse[h]).  The same tiles as above with the operands exchanged:
 // heads are the matrix rows, cache rows the columns, so a lane holds 16 heads of one cache row and adds them up by itself.
+template <int W, bool PAGED, bool WIDE>
 __global__ __launch_bounds__(256, 1) void kv4_probs_kernel(Kv4AttnArgs a)
 {
-    __shared__ __attribute__((aligned(16))) unsigned char ring[4][kRing][kTileB];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __shared__ __attribute__((aligned(1024))) Tiles lds;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, g = lane >> 5;
-    const int64_t q = blockIdx.x / a.n_splits;
-    const int split = (int)(blockIdx.x - q * a.n_splits);
-    const int b = (int)(q / a.Tq);
-    const int len = seq_len(a.pv, b, a.Lk);
-    const int s0 = split * a.split_len, s1 = min(s0 + a.split_len, a.k_sel);
-    const int32_t *idx = a.idx + q * a.k_sel;
-    const unsigned char *kv4 = (const unsigned char *)a.KV4;
+    const int nq = a.B * a.Tq;
+    const int wg = (int)blockIdx.x, wgs = (int)gridDim.x;
+    const int q0 = W > 1 ? wg / a.n_splits : (wgs & 7) == 0 ? ((wg & 7) * (wgs >> 3) + (wg >> 3)) * 4 + wave : wg * 4 + wave;
+    const int split = W > 1 ? wg - q0 * a.n_splits : 0;
+    if (W == 1 && q0 >= nq) return;
+    Fetch<W, PAGED, WIDE> f(a, lds, wave, q0, wgs * 4, split, W == 1 ? 0 : wave);
+    unsigned int n = 0, ok[3];
+    f.begin(lane, ok);
+    const float inv_h = 1.f / (float)a.H_q;
+#pragma unroll 1
+  for (int q = q0; q < nq; q += f.stride) {
     bf16x8 ql[8][4], qr[4];
     float off[16];                              // of head 8 (i / 4) + 4 g + i % 4, log2 units
     {
-        const unsigned short *qp = (const unsigned short *)a.Q + (q * a.H_q + (l32 < a.H_q ? l32 : 0)) * kRow;
+        const unsigned short *qp = (const unsigned short *)a.Q + ((int64_t)q * a.H_q + (l32 < a.H_q ? l32 : 0)) * kRow;
 #pragma unroll
         for (int j = 0; j < 8; ++j)
 #pragma unroll
@@ -614,56 +821,55 @@ __global__ __launch_bounds__(256, 1) void kv4_probs_kernel(Kv4AttnArgs a)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             const int h = 8 * (i >> 2) + 4 * g + (i & 3);
-            off[i] = h < a.H_q ? a.lse[q * a.H_q + h] * 1.4426950408889634f : INFINITY;
+            const float x = a.lse[(int64_t)q * a.H_q + min(h, a.H_q - 1)];
+            off[i] = h < a.H_q ? x * 1.4426950408889634f : INFINITY;
         }
     }
-    const float inv_h = 1.f / (float)a.H_q;
-    auto row_of = [&](int tile) -> int {
-        const int s = s0 + tile * kT + l32;
-        if (s >= s1) return -1;
-        return (int)kv4_row(a.pv, b, idx[s], len, a.Lk, a.pool_rows);
-    };
-    const int n_tiles = (s1 - s0 + kT - 1) / kT;
-    const unsigned int ring0 = (unsigned)__builtin_amdgcn_readfirstlane((int)lds_offset(&ring[wave][0][0]));
-    int row0 = wave < n_tiles ? row_of(wave) : -1, row1 = wave + 4 < n_tiles ? row_of(wave + 4) : -1;
-    fetch_tile(kv4, row0, ring0, lane);
-    fetch_tile(kv4, row1, ring0 + kTileB, lane);
-    unsigned int rat = 0, rat2 = 2 * kTileB;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) asm volatile("" : "+v"(ql[j][0]), "+v"(ql[j][1]), "+v"(ql[j][2]), "+v"(ql[j][3]));
+    asm volatile("" : "+v"(qr[0]), "+v"(qr[1]), "+v"(qr[2]), "+v"(qr[3]));
+#pragma unroll
+    for (int i = 0; i < 16; ++i) asm volatile("" : "+v"(off[i]));
 #pragma unroll 1
-    for (int t = wave; t < n_tiles; t += 4) {
-        const int row2 = t + 8 < n_tiles ? row_of(t + 8) : -1;
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        fetch_tile(kv4, row2, ring0 + rat2, lane);
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * 16) : "memory");
-        const unsigned char *kp = &ring[wave][0][0] + rat + l32 * kRowB;
-        const unsigned int sc = *(const unsigned int *)(kp + kScaleOff);
+    for (int t = f.first; t < f.n_tiles; t += W, ++n) {
+        f.ask_codes(n + 2, lane);
+        f.ask_pages(n + 4, f.entry(n + 4, lane));
+        f.ask_ids(n + 6, lane);
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kAhead) : "memory");
+        const unsigned char *kp = &lds.code[wave][0][0] + (n & (kRing - 1)) * kCodeB + l32 * 256;
+        const unsigned int sc = lds.scale[wave][n & 3][l32];
         f32x16 s;
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const u32x4 c = *(const u32x4 *)(kp + (2 * j + g) * 16);
-            const float f = scale_of((sc >> (8 * (j >> 1))) & 255u);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ql[j][e], widen(c[e], f), s, 0, 0, 0);
-        }
-#pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const bf16x8 k = *(const bf16x8 *)(kp + kRopeOff + 32 * r + 16 * g);
+            const bf16x8 k = *(const bf16x8 *)(&lds.rope[wave][0] + l32 * 128 + (((2 * r + g) ^ (l32 >> 1 & 7)) << 4));
             s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qr[r], k, s, 0, 0, 0);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        f.ask_ropes(n + 1, lane);
+        const unsigned int have = ok[0];
+        ok[0] = ok[1];
+        ok[1] = ok[2];
+        ok[2] = f.find_rows(n + 3, f.entry(n + 3, lane), f.page(n + 3, lane), lane);
+        f.advance();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const u32x4 c = *(const u32x4 *)(kp + (((2 * j + g) ^ (l32 & 15)) << 4));
+            const float x = scale_of((sc >> (8 * (j >> 1))) & 255u);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ql[j][e], widen(c[e], x), s, 0, 0, 0);
         }
         float p = 0.f;
 #pragma unroll
         for (int i = 0; i < 16; ++i)
             if (off[i] != INFINITY) p += __builtin_amdgcn_exp2f(s[i] * a.scale_log2e - off[i]);
         p = half_sum(p);
-        const int at = s0 + t * kT + l32;
-        if (g == 0 && at < s1) a.probs[q * a.k_sel + at] = row0 >= 0 ? p * inv_h : 0.f;
-        row0 = row1;
-        row1 = row2;
-        rat = rat == 2 * kTileB ? 0 : rat + kTileB;
-        rat2 = rat2 == 2 * kTileB ? 0 : rat2 + kTileB;
+        const int at = t * kT + l32;
+        if (g == 0 && at < f.n_slots) a.probs[(int64_t)q * a.k_sel + f.s0 + at] = (have >> l32) & 1u ? p * inv_h : 0.f;
     }
+    if (W > 1) break;
+  }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
 
@@ -687,20 +893,25 @@ hipError_t launch_kv4_read(const Kv4RowsArgs &a, hipStream_t st)
     return hipGetLastError();
 }
 
-hipError_t launch_kv4_attn(const Kv4AttnArgs &a, bool together, hipStream_t st)
-{
-    const int64_t units = (int64_t)a.B * a.Tq * a.n_splits;
-    if (together)
-        hipLaunchKernelGGL((kv4_attn_kernel<4>), dim3((unsigned)units), dim3(256), 0, st, a);
-    else
-        hipLaunchKernelGGL((kv4_attn_kernel<1>), dim3((unsigned)std::min<int64_t>(256, (units + 3) / 4)), dim3(256), 0, st, a);
-    return hipGetLastError();
-}
+// Whether every row of the cache begins below 4 GB (with the bytes behind a row's beginning that are added to it).
+bool kv4_wide(const Kv4AttnArgs &a) { return (uint64_t)a.pool_rows * kRowB > 0xFFFFFFFFull; }
 
-hipError_t launch_kv4_probs(const Kv4AttnArgs &a, hipStream_t st)
-{
-    hipLaunchKernelGGL(kv4_probs_kernel, dim3((unsigned)((int64_t)a.B * a.Tq * a.n_splits)), dim3(256), 0, st, a);
-    return hipGetLastError();
-}
+#define IC_KV4_LAUNCH(KERNEL)                                                                                                   \
+    const int64_t units = (int64_t)a.B * a.Tq * a.n_splits;                                                                     \
+    const dim3 block(256), grid((unsigned)(together ? units : std::min<int64_t>(256, (units + 3) / 4)));                        \
+    const bool paged = a.pv.page_table != nullptr, wide = kv4_wide(a);                                                          \
+    if (together && paged && wide) hipLaunchKernelGGL((KERNEL<4, true, true>), grid, block, 0, st, a);                          \
+    else if (together && paged) hipLaunchKernelGGL((KERNEL<4, true, false>), grid, block, 0, st, a);                            \
+    else if (together && wide) hipLaunchKernelGGL((KERNEL<4, false, true>), grid, block, 0, st, a);                             \
+    else if (together) hipLaunchKernelGGL((KERNEL<4, false, false>), grid, block, 0, st, a);                                    \
+    else if (paged && wide) hipLaunchKernelGGL((KERNEL<1, true, true>), grid, block, 0, st, a);                                 \
+    else if (paged) hipLaunchKernelGGL((KERNEL<1, true, false>), grid, block, 0, st, a);                                        \
+    else if (wide) hipLaunchKernelGGL((KERNEL<1, false, true>), grid, block, 0, st, a);                                         \
+    else hipLaunchKernelGGL((KERNEL<1, false, false>), grid, block, 0, st, a);                                                  \
+    return hipGetLastError()
+
+hipError_t launch_kv4_attn(const Kv4AttnArgs &a, bool together, hipStream_t st) { IC_KV4_LAUNCH(kv4_attn_kernel); }
+hipError_t launch_kv4_probs(const Kv4AttnArgs &a, bool together, hipStream_t st) { IC_KV4_LAUNCH(kv4_probs_kernel); }
+#undef IC_KV4_LAUNCH
 
 } // namespace ic
