@@ -1599,20 +1599,19 @@ ic_status check_attn_kv4(const ic_attn_desc *d, const ic_paged_cache *pc, int64_
     if (d->d_qk != 576 || d->d_v != 512 || d->v_off != 0 || d->row_elems != 576)
         return fail(IC_ERR_UNSUPPORTED, "a 4-bit cache holds rows of 576 with values 0..511 (d_qk=%d d_v=%d v_off=%d row_elems=%d)", d->d_qk, d->d_v,
                     d->v_off, d->row_elems);
+    if (d->k_sel > 1 << 24) return fail(IC_ERR_UNSUPPORTED, "k_sel=%d exceeds %d", d->k_sel, 1 << 24);
     return check_kv4_cache(pc, d->B, d->Lk, pool_rows);
 }
 
-// Splits of a query.  A workgroup's four waves take a split together (their tiles meet in LDS) unless the queries alone give
-// every wave of the chip one of its own.
+// Splits of a query, so that few of them still use all 256 compute units; a split has a tile for each of a workgroup's waves.
 struct Kv4Splits {
     int n, len;
-    bool together;
     size_t o_bytes, bytes;
 };
 Kv4Splits kv4_splits(const ic_attn_desc *d)
 {
     const int64_t nq = (int64_t)d->B * d->Tq, tiles = (d->k_sel + 31) / 32;
-    Kv4Splits r = {1, (int)tiles * 32, nq < 1024, 0, 0};
+    Kv4Splits r = {1, (int)tiles * 32, 0, 0};
     if (nq < 256) {
         int64_t ns = 256 / nq, most = (tiles + 3) / 4;
         if (ns > most) ns = most;
@@ -1641,6 +1640,7 @@ ic::Kv4AttnArgs kv4_attn_args(const ic_attn_desc *d, const ic_paged_cache *pc, i
     a.H_q = d->H_q;
     a.k_sel = d->k_sel;
     a.scale_log2e = d->sm_scale * 1.4426950408889634f;
+    a.lag = d->k_sel <= 8192 ? 12.f : 0.f;
     a.pv = paged_view(pc);
     return a;
 }
@@ -1704,7 +1704,9 @@ ic_status ic_sparse_attn_kv4(const ic_attn_desc *d, const ic_paged_cache *pc, in
     hipError_t e;
     {
         ProfScope ps(2, st);
-        e = ic::launch_kv4_attn(a, sp.together, st);
+        // Four waves to a query while no compute unit has more than two queries (2048 rows each, 512 queries: 127 us against 141
+        // with a wave to a query; 640: 163 against 154; 1024: 230 against 197).
+        e = ic::launch_kv4_attn(a, (int64_t)d->B * d->Tq <= 512, st);
     }
     if (e != hipSuccess) return fail(IC_ERR_HIP, "4-bit attention launch failed: %s", hipGetErrorString(e));
     if (sp.n > 1) {
@@ -1740,7 +1742,7 @@ ic_status ic_attn_probs_kv4(const ic_attn_desc *d, const ic_paged_cache *pc, int
     const Kv4Splits sp = kv4_splits(d);
     a.n_splits = sp.n;
     a.split_len = sp.len;
-    hipError_t e = ic::launch_kv4_probs(a, sp.together, (hipStream_t)stream);
+    hipError_t e = ic::launch_kv4_probs(a, (int64_t)d->B * d->Tq < 1024, (hipStream_t)stream);
     if (e != hipSuccess) return fail(IC_ERR_HIP, "4-bit attention-probability launch failed: %s", hipGetErrorString(e));
     return IC_OK;
 }

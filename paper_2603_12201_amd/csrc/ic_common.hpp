@@ -225,6 +225,7 @@ struct Kv4AttnArgs {
     int32_t B, Tq, Lk, H_q, k_sel;
     int32_t n_splits, split_len;   // slots per split, a multiple of 32
     float scale_log2e;
+    float lag;                     // log2 units a row may exceed the softmax's reference before the sums are scaled anew
     PagedView pv;
 };
 

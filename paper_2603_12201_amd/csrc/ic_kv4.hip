@@ -9,12 +9,13 @@
 // and stands for c * 2^e_j: e_j is the least e with max |x| <= 6 * 2^e, held to [-100, 100].  Scales are powers of two so
 // that every value is a bf16 (2 significant bits) and nothing but the choice of c rounds: a reader multiplies exact values.
 // One scale for 128 features is what the product with V can afford: there it goes into P (below), once per block and row;
-// for N(0,1) features the relative error is 0.125, 0.117 with blocks of 32.
+// for N(0,1) features the relative error is 0.125, and 0.115 with blocks of 32.
 //
 //   kv4_write_kernel  one wave per row: 16 lanes a block, its maximum by data-parallel moves, codes by the converting
 //                     instruction (ties to the even code).  Bound by memory: 1152 bytes in, 400 out.
 //   kv4_read_kernel   the way back to bf16, exact.
-//   kv4_attn_kernel   O = softmax(sm_scale Q K^T) V over the rows that idx names.  See there.
+//   kv4_attn_kernel, kv4_attn_few_kernel
+//                     O = softmax(sm_scale Q K^T) V over the rows that idx names.  See there.
 //   kv4_probs_kernel  the heads' mean of that softmax per selected row, from the log-sum-exps.
 #include <algorithm>
 #include <cstddef>
@@ -29,6 +30,7 @@ typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
 typedef __attribute__((ext_vector_type(2))) int i32x2;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
+typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
 typedef __attribute__((ext_vector_type(2))) unsigned int u32x2;
 
 constexpr int kRowB = IC_KV4_ROW_BYTES;
@@ -161,13 +163,13 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4RowsArgs a)
 // Registers: 256 of O^T, 144 of Q and about 100 more: one wave per SIMD, which issues in order, so the 68 matrix instructions
 // of a tile (32 clocks each) have the rest, about 6 vector instructions each, dealt out between them by hand: a step multiplies
 // K of one tile and V of the tile before it, and works out the softmax of the former during the latter.
+// The reference of the softmax is the running maximum, but followed only when a row exceeds it by more than a.lag (log2
+// units): 12 while k_sel rows times 6 2^(100 + 12) is a float (k_sel <= 8192), 0 above.
 
 constexpr int kT = 32;                        // rows of a tile
 constexpr int kCodeB = kT * 256, kRopeB = kT * 128;
 constexpr int kRing = 4;                      // tiles whose codes are in LDS
 constexpr float kPBias = 100.f;               // P is held times 2^100
-constexpr float kLag = 12.f;                  // log2 units a row may exceed its reference before the sums are scaled anew: 2^(100 + 12 + 11)
-                                              // (2048 rows) is still a float
 constexpr int kAmount = (127 + 100) << 7;     // what the exponent byte b is subtracted from, as a bf16 exponent: (227 - b) << 7
 
 // What a wave has in LDS.  Rows lie 256 (128) bytes apart, so a row's 16-byte pieces are stored in an order of its own, piece c
@@ -175,14 +177,15 @@ constexpr int kAmount = (127 + 100) << 7;     // what the exponent byte b is sub
 // The transposing read takes matrix rows 0-3, 8-11, 16-19, 24-27 (or the others) together, so the matrix row m >= 16 is the
 // tile's row 16 + ((m - 16) ^ 4): those too are 16 different r % 16.
 struct Tiles {
+    static constexpr int kSlotB = kCodeB;     // from a tile of the ring to the next
     unsigned char code[4][kRing][kCodeB];     // [wave]
+    __device__ __forceinline__ unsigned char *codes(int wave) { return &code[wave][0][0]; }
     unsigned char rope[4][kRopeB];
     int32_t idx[4][8][kT], page[4][4][kT];    // of tile n in [n % 8], [n % 4]
     unsigned int scale[4][4][kT];             // the rows' four exponent bytes, tile n in [n % 4]
     unsigned short amount[4][2][4][2][16];    // what is subtracted from P: tile n in [n % 2][block][half][register of the accumulator]
     unsigned int code_at[4][4][8];            // where the rows of the tile that is asked for next are: row 4 i + k at [k][i],
     unsigned int rope_at[4][2][8][4];         // row 8 i + k at [n % 2][k][i]
-    float ml[4][2][32];
 };
 __device__ __forceinline__ int tile_row(int m) { return m ^ ((m & 16) >> 2); }
 
@@ -231,10 +234,10 @@ struct Cursor {
 };
 
 // W waves share a query: each takes every W-th tile.  WIDE: rows behind 4 GB, in the 32-bit offsets of the others they are not.
-template <int W, bool PAGED, bool WIDE>
+template <int W, bool PAGED, bool WIDE, typename LDS>
 struct Fetch {
     const Kv4AttnArgs &a;
-    Tiles &lds;
+    LDS &lds;
     unsigned int code0, rope0, idx0, page0, scale0;   // LDS addresses of this wave's
     int wave;
     int nq, stride;                           // (B Tq is below 2^30, a stride 1024 at most)
@@ -242,11 +245,11 @@ struct Fetch {
     Cursor rows, pages, ids;
     const int32_t *ids_at;                    // idx of the query at `ids`
 
-    __device__ __forceinline__ Fetch(const Kv4AttnArgs &a_, Tiles &lds_, int wave_, int q, int stride_, int split, int first_)
+    __device__ __forceinline__ Fetch(const Kv4AttnArgs &a_, LDS &lds_, int wave_, int q, int stride_, int split, int first_)
         : a(a_), lds(lds_), wave(wave_), nq(a_.B * a_.Tq), stride(stride_), first(first_)
     {
         auto at = [](const void *p) { return (unsigned)__builtin_amdgcn_readfirstlane((int)lds_offset(p)); };
-        code0 = at(&lds.code[wave][0][0]);
+        code0 = at(lds.codes(wave));
         rope0 = at(&lds.rope[wave][0]);
         idx0 = at(&lds.idx[wave][0][0]);
         page0 = at(&lds.page[wave][0][0]);
@@ -334,15 +337,15 @@ struct Fetch {
     __device__ __forceinline__ u32x4 code_rows(int i4, int lane) const { return *(const u32x4 *)&lds.code_at[wave][lane >> 4][4 * i4]; }
     static __device__ __forceinline__ unsigned int code_piece(int lane) { return 16u * ((lane & 15) ^ (lane >> 4)); }
     template <int I> __device__ __forceinline__ void ask_code(unsigned int to, unsigned int r, unsigned int piece) const { ask16<I * 1024>(r, piece ^ (64u * (I & 3)), to); }
-    __device__ __forceinline__ unsigned int code_slot(unsigned int m) const { return code0 + (m & (kRing - 1)) * kCodeB; }
+    __device__ __forceinline__ unsigned int code_slot(unsigned int m) const { return code0 + (m & (kRing - 1)) * LDS::kSlotB; }
     // eight rows' rotary parts, 8 lanes each: row 8 i + lane / 8
     __device__ __forceinline__ u32x4 rope_rows(unsigned int m, int lane) const { return *(const u32x4 *)&lds.rope_at[wave][m & 1][lane >> 3][0]; }
     static __device__ __forceinline__ unsigned int rope_piece(int lane) { return kRopeOff + 16u * ((lane & 7) ^ (lane >> 4)); }
     template <int I> __device__ __forceinline__ void ask_rope(unsigned int r, unsigned int piece) const { ask16<I * 1024>(r, piece ^ (64u * (I & 1)), rope0); }
-    __device__ __forceinline__ void ask_codes(unsigned int m, int lane) const
+    __device__ __forceinline__ void ask_codes(unsigned int to, int lane) const
     {
         const u32x4 r0 = code_rows(0, lane), r1 = code_rows(1, lane);
-        const unsigned int to = code_slot(m), piece = code_piece(lane);
+        const unsigned int piece = code_piece(lane);
         ask_code<0>(to, r0[0], piece);
         ask_code<1>(to, r0[1], piece);
         ask_code<2>(to, r0[2], piece);
@@ -380,7 +383,7 @@ struct Fetch {
         for (unsigned int i = 0; i < 3; ++i) {
             ok[i] = find_rows(i, entry(i, lane), page(i, lane), lane);
             next(rows);
-            if (i < 2) ask_codes(i, lane);
+            if (i < 2) ask_codes(code_slot(i), lane);
             if (i == 0) ask_ropes(0, lane);
         }
         asm volatile("s_waitcnt vmcnt(10)" ::: "memory");                   // (tile 0 has arrived)
@@ -401,10 +404,10 @@ __device__ __forceinline__ float half_sum(float x)
 
 // O^T times a factor per head, a tile at a time: the accumulators live in registers that only matrix instructions and moves
 // reach, and all of them out at once would displace everything else.
-__device__ __forceinline__ void scale_tiles(f32x16 (&o)[16], float f)
+template <int N> __device__ __forceinline__ void scale_tiles(f32x16 (&o)[N], float f)
 {
 #pragma unroll
-    for (int t = 0; t < 16; ++t) {
+    for (int t = 0; t < N; ++t) {
         f32x16 y = o[t];
         asm volatile("" : "+v"(y));
 #pragma unroll
@@ -436,19 +439,18 @@ __device__ __forceinline__ void mfma_new(f32x16 &s, bf16x8 x, bf16x8 y) { asm vo
 __device__ __forceinline__ void mfma_add(f32x16 &s, bf16x8 x, bf16x8 y) { asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(x), "v"(y)); }
 __device__ __forceinline__ void mfma_settle(f32x16 &s) { asm volatile("s_nop 13" : "+v"(s)); }
 
-// W waves of the workgroup share a (query, split): each takes every W-th tile and they meet at the end.
-template <int W, bool PAGED, bool WIDE>
+// Many queries: each of the 1024 waves has queries of its own, one after the other.
+template <bool PAGED, bool WIDE>
 __global__ __launch_bounds__(256, 1) void kv4_attn_kernel(Kv4AttnArgs a)
 {
     __shared__ __attribute__((aligned(1024))) Tiles lds;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int nq = a.B * a.Tq;
-    // W = 1: the waves of an XCD (every eighth workgroup) walk through neighbouring queries, whose selections overlap
+    // the waves of an XCD (every eighth workgroup) walk through neighbouring queries, whose selections overlap
     const int wg = (int)blockIdx.x, wgs = (int)gridDim.x;
-    const int q0 = W > 1 ? wg / a.n_splits : (wgs & 7) == 0 ? ((wg & 7) * (wgs >> 3) + (wg >> 3)) * 4 + wave : wg * 4 + wave;
-    const int split = W > 1 ? wg - q0 * a.n_splits : 0;
-    if (W == 1 && q0 >= nq) return;
-    Fetch<W, PAGED, WIDE> f(a, lds, wave, q0, wgs * 4, split, W == 1 ? 0 : wave);
+    const int q0 = (wgs & 7) == 0 ? ((wg & 7) * (wgs >> 3) + (wg >> 3)) * 4 + wave : wg * 4 + wave;
+    if (q0 >= nq) return;
+    Fetch<1, PAGED, WIDE, Tiles> f(a, lds, wave, q0, wgs * 4, 0, 0);
     unsigned int n = 0, ok[3];                 // tile number; which rows it and the next two have
     f.begin(lane_now(), ok);
 #pragma unroll 1
@@ -538,7 +540,7 @@ __global__ __launch_bounds__(256, 1) void kv4_attn_kernel(Kv4AttnArgs a)
         sc = lds.scale[wave][n & 3][kr];
     }
 #pragma unroll 1
-    for (int t = f.first; t < f.n_tiles; t += W, ++n) {
+    for (int t = 0; t < f.n_tiles; ++t, ++n) {
         if (anew) scale_tiles(o, keep);
 #pragma unroll
         for (int t2 = 0; t2 < 16; ++t2) asm volatile("" : "+a"(o[t2]));
@@ -553,7 +555,7 @@ __global__ __launch_bounds__(256, 1) void kv4_attn_kernel(Kv4AttnArgs a)
         const unsigned char *const vrow = v_at(m1, vr, ln);
         if (ok[0] == 0u) {
             // no rows: nothing to score; the tile before may wait for its product
-            f.ask_codes(n + 2, ln);
+            f.ask_codes(f.code_slot(n + 2), ln);
             f.ask_pages(n + 4, f.entry(n + 4, ln));
             f.ask_ids(n + 6, ln);
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kAhead) : "memory");
@@ -664,7 +666,7 @@ __global__ __launch_bounds__(256, 1) void kv4_attn_kernel(Kv4AttnArgs a)
             if (i == 7) f.template ask_rope<3>(ro[3], rpiece);
             if (i == 9) {
                 top = half_max(top) * a.scale_log2e;
-                anew = __ballot(top > m + kLag) != 0ull;                    // (m = -inf: the first rows)
+                anew = __ballot(top > m + a.lag) != 0ull;                    // (m = -inf: the first rows)
             }
             if (i == 10) {
                 const float mn = anew ? fmaxf(m, top) : m;
@@ -704,86 +706,255 @@ __global__ __launch_bounds__(256, 1) void kv4_attn_kernel(Kv4AttnArgs a)
     const int lane = lane_now(), l32 = lane & 31, g = lane >> 5;
     l = half_sum(l);
 
-    float mine = 1.f;                          // weight of this wave's part
-    if constexpr (W > 1) {
-        // the waves' parts: weights by their maxima, then each wave sums a quarter of the features, in two rounds through the rings
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                    // nothing more arrives in the rings
-        __syncthreads();
-        if (g == 0) {
-            lds.ml[wave][0][l32] = m;
-            lds.ml[wave][1][l32] = l;
-        }
-        __syncthreads();
-        float mt = -INFINITY, lt = 0.f;
-#pragma unroll
-        for (int w = 0; w < W; ++w) mt = fmaxf(mt, lds.ml[w][0][l32]);
-#pragma unroll
-        for (int w = 0; w < W; ++w) {
-            const float mw = lds.ml[w][0][l32];
-            lt += mw == -INFINITY ? 0.f * lds.ml[w][1][l32] : lds.ml[w][1][l32] * __builtin_amdgcn_exp2f(mw - mt);
-        }
-        mine = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mt);
-        m = mt;
-        l = lt;
-    }
     const float inv = l == 0.f ? 0.f : 0x1p100f / l;                        // (the sums of P V are without the bias)
-    const bool mine_h = l32 < a.H_q;
-    const int64_t head = (int64_t)q * a.H_q + l32, part = ((int64_t)q * a.n_splits + split) * a.H_q + l32;
-    // features 32 ft + 8 i4 + 4 g + 0 .. 3 of the head
-    auto store = [&](int ft, int i4, f32x4 y) __attribute__((always_inline)) {
-        const int f = 32 * ft + 8 * i4 + 4 * g;
-        if (!mine_h) return;
-        if (W > 1 && a.n_splits > 1) {
-            *(f32x4 *)((float *)a.part_o + part * kLat + f) = y * inv;
-        } else {
-            typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
-            *(bf16x4 *)((__bf16 *)a.O + head * kLat + f) = __builtin_convertvector(y * inv, bf16x4);
-        }
-    };
-    if constexpr (W == 1) {
+    const int64_t head = (int64_t)q * a.H_q + l32;
+    if (l32 < a.H_q) {
+        // features 32 ft + 8 i4 + 4 g + 0 .. 3 of the head
 #pragma unroll
         for (int ft = 0; ft < 16; ++ft)
 #pragma unroll
-            for (int i4 = 0; i4 < 4; ++i4) store(ft, i4, read4(o[ft], i4, 1.f));
-    } else {
-        f32x4 *sh = (f32x4 *)&lds.code[0][0][0];   // [from][owner][tile of the round][register / 4][lane]
-#pragma unroll
-        for (int round = 0; round < 2; ++round) {
-#pragma unroll
-            for (int w = 0; w < W; ++w)
-                if (w != wave)
-#pragma unroll
-                    for (int k = 0; k < 2; ++k)
-#pragma unroll
-                        for (int i4 = 0; i4 < 4; ++i4) sh[(((wave * 4 + w) * 2 + k) * 4 + i4) * 64 + lane] = read4(o[4 * w + 2 * round + k], i4, mine);
-            __syncthreads();
-#pragma unroll
-            for (int w = 0; w < W; ++w)
-                if (w == wave)
-#pragma unroll
-                    for (int k = 0; k < 2; ++k)
-#pragma unroll
-                        for (int i4 = 0; i4 < 4; ++i4) {
-                            f32x4 x = read4(o[4 * w + 2 * round + k], i4, mine);
-#pragma unroll
-                            for (int from = 0; from < W; ++from)
-                                if (from != w) x += sh[(((from * 4 + w) * 2 + k) * 4 + i4) * 64 + lane];
-                            store(4 * w + 2 * round + k, i4, x);
-                        }
-            if (round == 0) __syncthreads();
-        }
+            for (int i4 = 0; i4 < 4; ++i4)
+                *(bf16x4 *)((__bf16 *)a.O + head * kLat + 32 * ft + 8 * i4 + 4 * g) = __builtin_convertvector(read4(o[ft], i4, inv), bf16x4);
+        if (g == 0 && a.lse) a.lse[head] = l == 0.f ? -INFINITY : (m + __builtin_log2f(l) - kPBias) * 0.6931471805599453f;
     }
-    if (g == 0 && mine_h && (W == 1 || wave == 0)) {
-        if (W > 1 && a.n_splits > 1) {
-            a.part_ml[2 * part] = l == 0.f ? -INFINITY : (l != l ? l : m);   // (the merge leaves out what has no maximum)
-            a.part_ml[2 * part + 1] = l * 0x1p-100f;
-        } else if (a.lse) {
-            a.lse[head] = l == 0.f ? -INFINITY : (m + __builtin_log2f(l) - kPBias) * 0.6931471805599453f;
-        }
-    }
-    if (W > 1) break;                          // (one query)
   }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+}
+
+// Few queries: the four waves of a workgroup share one, or a split of one.  In a step each scores a tile; they agree on the
+// reference by the four tiles' maxima, and each multiplies all four tiles' P with its own 128 features of V, which are one
+// block: its sums of O are 64 registers, and there is nothing to add up between the waves at the end (with a tile's product
+// to itself each wave had all 512 features, and their sum through LDS took 10 000 clocks).  What bounds a launch is latency:
+// entries, page numbers and rows from memory one after the other, Q meanwhile (36 KB, once in LDS for all four waves: read
+// by each from memory it took 9 000 clocks), then 2.8 us a step of 128 rows.  Measured back to back in a graph: 32 rows of one
+// query 8.4 us (15.3 before these two), 2048 rows in 16 splits 13.4 with their merge, 40 queries of 2048 rows 24.9.
+struct FewTiles {
+    static constexpr int kSlotB = 4 * kCodeB;
+    unsigned char code[3][4][kCodeB];         // [ring][wave]
+    u32x4 p[2][4][2][64];                     // P: step n in [n % 2][wave][registers 0-3, 4-7 (rows in pairs)][lane]; at first Q, from code[2] on
+    unsigned char rope[4][kRopeB];
+    int32_t idx[4][8][kT], page[4][4][kT];
+    unsigned int scale[4][4][kT];
+    unsigned short amount[2][4][4][2][16];    // [n % 2][wave][block][half][register]
+    unsigned int code_at[4][4][8], rope_at[4][2][8][4];
+    float top[2][4][32], sum[4][32];
+    __device__ __forceinline__ unsigned char *codes(int wave) { return &code[0][wave][0]; }
+};
+
+// LDS writes are there for the workgroup's other waves, reads are done.  (No wait for what is on its way from memory.)
+__device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// Q into LDS, a quarter of the heads per wave: head h 1152 h bytes on, its 16-byte piece c at c ^ (h / 2 % 8) (16 heads' pieces are
+// then in 16 different bank groups).  Nine instructions.
+__device__ __forceinline__ void ask_q(const Kv4AttnArgs &a, int q, unsigned int lds, int wave, int lane)
+{
+#pragma unroll
+    for (int i = 0; i < 9; ++i) {
+        const int at = 576 * wave + 64 * i + lane, h = at / 72, c = at - 72 * h;
+        to_lds16((const unsigned char *)a.Q + (((int64_t)q * a.H_q + (h < a.H_q ? h : 0)) * (2 * kRow) + 16 * (c ^ (h >> 1 & 7))), lds + 16 * (576 * wave + 64 * i), 0);
+    }
+}
+// A lane's pieces of it: head lane & 31; chunk j, step s: features 64 j + 32 g + 8 s ..; then the rotary ones, 16 r + 8 g ..
+__device__ __forceinline__ void read_q(const unsigned char *lds, int lane, bf16x8 (&ql)[8][4], bf16x8 (&qr)[4])
+{
+    const int h = lane & 31, g = lane >> 5, x = h >> 1 & 7;
+    const unsigned char *row = lds + h * (2 * kRow);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int s = 0; s < 4; ++s) ql[j][s] = *(const bf16x8 *)(row + 16 * ((8 * j + 4 * g + s) ^ x));
+#pragma unroll
+    for (int r = 0; r < 4; ++r) qr[r] = *(const bf16x8 *)(row + 16 * ((64 + 2 * r + g) ^ x));
+}
+
+template <bool PAGED, bool WIDE>
+__global__ __launch_bounds__(256, 1) void kv4_attn_few_kernel(Kv4AttnArgs a)
+{
+    __shared__ __attribute__((aligned(1024))) FewTiles lds;
+    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int l32 = lane & 31, g = lane >> 5;
+    const int q = (int)blockIdx.x / a.n_splits, split = (int)blockIdx.x - q * a.n_splits;
+    Fetch<4, PAGED, WIDE, FewTiles> f(a, lds, wave, q, 0, split, wave);
+    static_assert(sizeof(lds.code[2]) + sizeof(lds.p) >= 32 * 2 * kRow, "Q");
+    unsigned char *const q_lds = &lds.code[2][0][0];
+    ask_q(a, q, (unsigned)__builtin_amdgcn_readfirstlane((int)lds_offset(q_lds)), wave, lane);
+    unsigned int n = 0, slot = 0, ok[3];
+    f.begin(lane, ok);
+    meet();                                    // (Q was asked for before what begin() has waited for)
+    bf16x8 ql[8][4], qr[4];
+    read_q(q_lds, lane, ql, qr);
+    f32x16 o[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
+    float m = -INFINITY, l = 0.f;
+    const int kr = tile_row(l32), gr = 16 * (g ^ (kr & 15)), rr = 16 * (g ^ (kr >> 1 & 7));
+    const int vr = tile_row(8 * ((lane & 15) >> 2) + 4 * g + (lane & 3)), r16 = 16 * (vr & 15);
+    const int n_steps = (f.n_tiles + 3) / 4;
+    auto k_at = [&](unsigned int at) __attribute__((always_inline)) { return &lds.code[at][wave][kr * 256]; };
+    u32x4 kc[3];                               // K's codes, chunks j in [j % 3]; of the tile that comes 0 and 1, and its exponents
+    kc[0] = *(const u32x4 *)(k_at(0) + gr);
+    kc[1] = *(const u32x4 *)(k_at(0) + (32 ^ gr));
+    unsigned int sc = lds.scale[wave][0][kr];
+    auto pin = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) asm volatile("" : "+v"(ql[j][0]), "+v"(ql[j][1]), "+v"(ql[j][2]), "+v"(ql[j][3]));
+        asm volatile("" : "+v"(qr[0]), "+v"(qr[1]), "+v"(qr[2]), "+v"(qr[3]));
+    };
+    pin();
+#pragma unroll 1
+    for (int t = 0; t < n_steps; ++t, ++n) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm volatile("" : "+a"(o[i]));
+        pin();
+        // S = K Q^T of this wave's tile
+        f32x16 s;
+        if (ok[0] == 0u) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = -INFINITY;
+            asm volatile("s_waitcnt vmcnt(11)" ::: "memory");
+        } else {
+            const unsigned char *const krow = k_at(slot), *const rrow = &lds.rope[wave][kr * 128];
+            bf16x8 kb[3], rk[3];
+            float sf[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sf[j] = scale_of((sc >> (8 * j)) & 255u);
+            kb[0] = widen(kc[0][0], sf[0]);
+            kb[1] = widen(kc[0][1], sf[0]);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                const int j = i >> 2, e = i & 3;
+                if (i == 0)
+                    mfma_new(s, kb[0], ql[0][0]);
+                else
+                    mfma_add(s, kb[i % 3], ql[j][e]);
+                __builtin_amdgcn_sched_barrier(0);
+                if (i < 30) kb[(i + 2) % 3] = widen(kc[((i + 2) >> 2) % 3][(i + 2) & 3], sf[(i + 2) >> 3]);
+                if (e == 0 && j < 6) kc[(j + 2) % 3] = *(const u32x4 *)(krow + ((32 * (j + 2)) ^ gr));
+                if (i >= 2 && i < 6)
+                    lds.amount[n & 1][wave][i - 2][(l32 >> 2) & 1][4 * (l32 >> 3) + (l32 & 3)] = (unsigned short)(kAmount - (int)(((sc >> (8 * (i - 2))) & 255u) << 7));
+                if (i == 25) asm volatile("s_waitcnt vmcnt(11)" ::: "memory");  // (what was asked for behind the rotary part)
+                if (i >= 26 && i < 29) rk[i - 26] = *(const bf16x8 *)(rrow + ((32 * (i - 26)) ^ rr));
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                mfma_add(s, rk[r % 3], qr[r]);
+                __builtin_amdgcn_sched_barrier(0);
+                if (r == 0) rk[0] = *(const bf16x8 *)(rrow + (96 ^ rr));
+            }
+            mfma_settle(s);
+            if (ok[0] != 0xFFFFFFFFu) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int tr = 8 * (i >> 2) + 4 * (i < 8 ? g : 1 - g) + (i & 3);
+                    s[i] = (ok[0] >> tr) & 1u ? s[i] : -INFINITY;
+                }
+            }
+        }
+        float top = fmaxf(s[0], s[1]);
+#pragma unroll
+        for (int i = 2; i < 16; i += 2) top = fmaxf(fmaxf(top, s[i]), s[i + 1]);
+        top = half_max(top) * a.scale_log2e;
+        lds.top[n & 1][wave][l32] = top;
+        meet();
+        // (everybody is through the step before: the ring's third tile is free)
+        float tops[4];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) tops[w] = lds.top[n & 1][w][l32];
+        const unsigned int two = slot == 0 ? 2 : slot - 1;
+        f.ask_ropes(n + 1, lane);
+        f.ask_codes((unsigned)__builtin_amdgcn_readfirstlane((int)(f.code0 + two * FewTiles::kSlotB)), lane);
+        f.ask_pages(n + 4, f.entry(n + 4, lane));
+        f.ask_ids(n + 6, lane);
+        top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+        if (__ballot(top > m + a.lag) != 0ull) {                             // (the same in every wave)
+            const float mn = fmaxf(m, top), keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+            m = mn;
+            l *= keep;
+            scale_tiles(o, keep);
+        }
+        const float ref = m == -INFINITY ? 0.f : m - kPBias;
+        u32x4 p[2];
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) {
+            const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.scale_log2e, -ref)), p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i + 1], a.scale_log2e, -ref));
+            l += p0 + p1;
+            p[i >> 3][(i >> 1) & 3] = __builtin_bit_cast(unsigned int, __builtin_convertvector((f32x2{p0, p1}), bf16x2));
+        }
+        lds.p[n & 1][wave][0][lane] = p[0];
+        lds.p[n & 1][wave][1][lane] = p[1];
+        ok[0] = ok[1];
+        ok[1] = ok[2];
+        asm volatile("s_waitcnt vmcnt(14)" ::: "memory");                   // (this step's: the page numbers of n + 3 were asked for a step ago)
+        ok[2] = f.find_rows(n + 3, f.entry(n + 3, lane), f.page(n + 3, lane), lane);
+        f.advance();
+        meet();
+        // O^T += V^T P^T of the four tiles, this wave's features.  (A tile without rows: its P is 0, and any code is a number.)
+        typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
+        u32x4 pv[2][2], am[2][2];
+        i32x2 vc[2][4];
+        const unsigned char *const vrow = &lds.code[slot][0][vr * 256 + ((lane >> 4) & 1) * 8];
+        auto v_get = [&](int w) __attribute__((always_inline)) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                pv[w & 1][h] = lds.p[n & 1][w][h][lane];
+                am[w & 1][h] = *(const u32x4 *)&lds.amount[n & 1][w][wave][g][8 * h];
+            }
+#pragma unroll
+            for (int t4 = 0; t4 < 4; ++t4) vc[w & 1][t4] = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2 *)(vrow + w * kCodeB + ((64 * wave + 16 * t4) ^ r16)));
+        };
+        v_get(0);
+        slot = slot == 2 ? 0 : slot + 1;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            if (4 * t + w >= f.n_tiles) break;
+            if (w < 3) v_get(w + 1);
+            if (w == 3) {
+                kc[0] = *(const u32x4 *)(k_at(slot) + gr);
+                kc[1] = *(const u32x4 *)(k_at(slot) + (32 ^ gr));
+                sc = lds.scale[wave][(n + 1) & 3][kr];
+            }
+            u32x4 pj[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    pj[h][i] = __builtin_bit_cast(unsigned int, __builtin_elementwise_sub_sat(as_u16x2(pv[w & 1][h][i]), as_u16x2(am[w & 1][h][i])));
+#pragma unroll
+            for (int t4 = 0; t4 < 4; ++t4) {
+                const i32x2 c = vc[w & 1][t4];
+                o[t4] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen((unsigned)c[0], 1.f), __builtin_bit_cast(bf16x8, pj[0]), o[t4], 0, 0, 0);
+                o[t4] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen((unsigned)c[1], 1.f), __builtin_bit_cast(bf16x8, pj[1]), o[t4], 0, 0, 0);
+            }
+        }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    lds.sum[wave][l32] = half_sum(l);
+    meet();
+    l = (lds.sum[0][l32] + lds.sum[1][l32]) + (lds.sum[2][l32] + lds.sum[3][l32]);
+    if (l32 >= a.H_q) return;
+    const float inv = l == 0.f ? 0.f : 0x1p100f / l;
+    const int64_t head = (int64_t)q * a.H_q + l32, part = ((int64_t)q * a.n_splits + split) * a.H_q + l32;
+#pragma unroll
+    for (int t4 = 0; t4 < 4; ++t4)
+#pragma unroll
+        for (int i4 = 0; i4 < 4; ++i4) {
+            const f32x4 y = f32x4{o[t4][4 * i4], o[t4][4 * i4 + 1], o[t4][4 * i4 + 2], o[t4][4 * i4 + 3]} * inv;
+            const int at = 128 * wave + 32 * t4 + 8 * i4 + 4 * g;
+            if (a.n_splits > 1)
+                *(f32x4 *)((float *)a.part_o + part * kLat + at) = y;
+            else
+                *(bf16x4 *)((__bf16 *)a.O + head * kLat + at) = __builtin_convertvector(y, bf16x4);
+        }
+    if (g != 0 || wave != 0) return;
+    if (a.n_splits > 1) {
+        a.part_ml[2 * part] = l == 0.f ? -INFINITY : (l != l ? l : m);       // (the merge leaves out what has no maximum)
+        a.part_ml[2 * part + 1] = l * 0x1p-100f;
+    } else if (a.lse) {
+        a.lse[head] = l == 0.f ? -INFINITY : (m + __builtin_log2f(l) - kPBias) * 0.6931471805599453f;
+    }
 }
 
 // ---- the weight each selected row received --------------------------------------------------------------------------
@@ -801,7 +972,7 @@ __global__ __launch_bounds__(256, 1) void kv4_probs_kernel(Kv4AttnArgs a)
     const int q0 = W > 1 ? wg / a.n_splits : (wgs & 7) == 0 ? ((wg & 7) * (wgs >> 3) + (wg >> 3)) * 4 + wave : wg * 4 + wave;
     const int split = W > 1 ? wg - q0 * a.n_splits : 0;
     if (W == 1 && q0 >= nq) return;
-    Fetch<W, PAGED, WIDE> f(a, lds, wave, q0, wgs * 4, split, W == 1 ? 0 : wave);
+    Fetch<W, PAGED, WIDE, Tiles> f(a, lds, wave, q0, wgs * 4, split, W == 1 ? 0 : wave);
     unsigned int n = 0, ok[3];
     f.begin(lane, ok);
     const float inv_h = 1.f / (float)a.H_q;
@@ -832,7 +1003,7 @@ __global__ __launch_bounds__(256, 1) void kv4_probs_kernel(Kv4AttnArgs a)
     for (int i = 0; i < 16; ++i) asm volatile("" : "+v"(off[i]));
 #pragma unroll 1
     for (int t = f.first; t < f.n_tiles; t += W, ++n) {
-        f.ask_codes(n + 2, lane);
+        f.ask_codes(f.code_slot(n + 2), lane);
         f.ask_pages(n + 4, f.entry(n + 4, lane));
         f.ask_ids(n + 6, lane);
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kAhead) : "memory");
@@ -896,22 +1067,39 @@ hipError_t launch_kv4_read(const Kv4RowsArgs &a, hipStream_t st)
 // Whether every row of the cache begins below 4 GB (with the bytes behind a row's beginning that are added to it).
 bool kv4_wide(const Kv4AttnArgs &a) { return (uint64_t)a.pool_rows * kRowB > 0xFFFFFFFFull; }
 
-#define IC_KV4_LAUNCH(KERNEL)                                                                                                   \
-    const int64_t units = (int64_t)a.B * a.Tq * a.n_splits;                                                                     \
-    const dim3 block(256), grid((unsigned)(together ? units : std::min<int64_t>(256, (units + 3) / 4)));                        \
-    const bool paged = a.pv.page_table != nullptr, wide = kv4_wide(a);                                                          \
-    if (together && paged && wide) hipLaunchKernelGGL((KERNEL<4, true, true>), grid, block, 0, st, a);                          \
-    else if (together && paged) hipLaunchKernelGGL((KERNEL<4, true, false>), grid, block, 0, st, a);                            \
-    else if (together && wide) hipLaunchKernelGGL((KERNEL<4, false, true>), grid, block, 0, st, a);                             \
-    else if (together) hipLaunchKernelGGL((KERNEL<4, false, false>), grid, block, 0, st, a);                                    \
-    else if (paged && wide) hipLaunchKernelGGL((KERNEL<1, true, true>), grid, block, 0, st, a);                                 \
-    else if (paged) hipLaunchKernelGGL((KERNEL<1, true, false>), grid, block, 0, st, a);                                        \
-    else if (wide) hipLaunchKernelGGL((KERNEL<1, false, true>), grid, block, 0, st, a);                                         \
-    else hipLaunchKernelGGL((KERNEL<1, false, false>), grid, block, 0, st, a);                                                  \
-    return hipGetLastError()
+// Kernel forms by what a cache is.
+#define IC_KV4_FORMS(KERNEL, GRID)                                                                                              \
+    do {                                                                                                                        \
+        const dim3 block(256), grid((unsigned)(GRID));                                                                          \
+        const bool paged = a.pv.page_table != nullptr, wide = kv4_wide(a);                                                      \
+        if (paged && wide) hipLaunchKernelGGL((KERNEL(true, true)), grid, block, 0, st, a);                                     \
+        else if (paged) hipLaunchKernelGGL((KERNEL(true, false)), grid, block, 0, st, a);                                       \
+        else if (wide) hipLaunchKernelGGL((KERNEL(false, true)), grid, block, 0, st, a);                                        \
+        else hipLaunchKernelGGL((KERNEL(false, false)), grid, block, 0, st, a);                                                 \
+    } while (0)
+#define IC_KV4_MANY(P, L) kv4_attn_kernel<P, L>
+#define IC_KV4_FEW(P, L) kv4_attn_few_kernel<P, L>
+#define IC_KV4_PROBS1(P, L) kv4_probs_kernel<1, P, L>
+#define IC_KV4_PROBS4(P, L) kv4_probs_kernel<4, P, L>
 
-hipError_t launch_kv4_attn(const Kv4AttnArgs &a, bool together, hipStream_t st) { IC_KV4_LAUNCH(kv4_attn_kernel); }
-hipError_t launch_kv4_probs(const Kv4AttnArgs &a, bool together, hipStream_t st) { IC_KV4_LAUNCH(kv4_probs_kernel); }
-#undef IC_KV4_LAUNCH
+hipError_t launch_kv4_attn(const Kv4AttnArgs &a, bool together, hipStream_t st)
+{
+    const int64_t units = (int64_t)a.B * a.Tq * a.n_splits;
+    if (together)
+        IC_KV4_FORMS(IC_KV4_FEW, units);
+    else
+        IC_KV4_FORMS(IC_KV4_MANY, std::min<int64_t>(256, (units + 3) / 4));
+    return hipGetLastError();
+}
+
+hipError_t launch_kv4_probs(const Kv4AttnArgs &a, bool together, hipStream_t st)
+{
+    const int64_t units = (int64_t)a.B * a.Tq * a.n_splits;
+    if (together)
+        IC_KV4_FORMS(IC_KV4_PROBS4, units);
+    else
+        IC_KV4_FORMS(IC_KV4_PROBS1, std::min<int64_t>(256, (units + 3) / 4));
+    return hipGetLastError();
+}
 
 } // namespace ic

@@ -336,6 +336,30 @@ def test_wide_scales(ic):
     check_query(O[0, 0], lse[0, 0], None, kv4_ref.bf16_bits_to_f64(bits(Q))[0, 0], kv4_ref.unpack(kv4.cpu().numpy()[0]), np.ones(96, dtype=bool))
 
 
+@pytest.mark.parametrize("nq", [1, 300, 700])
+def test_many_slots_of_the_largest_values(ic, nq):
+    """16384 rows of 6 2^100, all but the first 128 of them 11.5 powers of two heavier: the sums must stay finite."""
+    say(f"16384 slots, {nq} queries")
+    k = 16384
+    packed = np.zeros((1, k, 400), dtype=np.uint8)
+    packed[..., :256] = 0x77
+    packed[..., 384:388] = 227
+    rope = torch.zeros((k, 64), dtype=torch.bfloat16)
+    rope[128:, 0] = 11.5 / (1.4427 * SCALE)
+    packed[0, :, 256:384] = rope.view(torch.uint8).numpy()
+    Q = torch.zeros((1, nq, 32, 576), dtype=torch.bfloat16)
+    Q[..., 512] = 1.0
+    idx = torch.arange(k, dtype=torch.int32, device="cuda").expand(1, nq, k).contiguous()
+    O, lse = ic.sparse_attn_kv4(Q.cuda(), torch.from_numpy(packed).cuda(), idx, SCALE, want_lse=True)
+    # every row holds the same value, and so does their mean, but for roundings: 2^-8 of each P, 2^-8 of O, and in the two
+    # sums, whose longest chains have 16384 / 2 and 16384 terms, at most 2^-11 and 2^-10
+    x = O.double().cpu().numpy() / (6.0 * 2.0 ** 100)
+    assert np.all(np.abs(x - 1.0) <= 2.0 ** -7 + 2.0 ** -9), (x.min(), x.max())
+    s = SCALE * rope[:, 0].double().numpy()
+    want = np.log(np.exp(s - s.max()).sum()) + s.max()
+    assert np.all(np.abs(lse.double().cpu().numpy() - want) <= 2.0 ** -11 + 2.0 ** -20 * (1 + want))
+
+
 def test_rows_behind_4_gib(ic):
     """A pool of 11.2 million rows (4.5 GB): row offsets pass 32 bits."""
     n = 175000 * 64
