@@ -403,6 +403,26 @@ def test_binding_refuses_mismatched_tensors(ic):
             pytest.fail("call %d went through" % i)
 
 
+def test_tensors_away_from_the_current_device_are_refused(ic, monkeypatch):
+    from paper_2603_12201_amd import binding
+    kv4 = torch.zeros((2, 64, 400), dtype=torch.uint8, device="cuda")
+    x = torch.zeros((2, 3, 576), dtype=torch.bfloat16, device="cuda")
+    Q = torch.zeros((2, 1, 32, 576), dtype=torch.bfloat16, device="cuda")
+    idx = torch.zeros((2, 1, 16), dtype=torch.int32, device="cuda")
+    lse, weight, keep = torch.zeros((2, 1, 32), device="cuda"), torch.zeros((2, 64), device="cuda"), torch.zeros((2, 8), dtype=torch.int32, device="cuda")
+    calls = [
+        lambda: ic.kv4_write(x, kv4), lambda: ic.kv4_read(kv4, 2, 2), lambda: ic.sparse_attn_kv4(Q, kv4, idx, SCALE),
+        lambda: ic.attn_probs_kv4(Q, kv4, idx, SCALE, lse), lambda: ic.attn_weight_add(torch.zeros((2, 1, 16), device="cuda"), idx, weight),
+        lambda: ic.evict_keep(weight, 8), lambda: ic.cache_compact([(kv4, kv4[:, :8].contiguous())], keep, 64),
+    ]
+    for f in calls:
+        f()
+    monkeypatch.setattr(binding, "_current_device", lambda: 1)
+    for f in calls:
+        with pytest.raises(ic.IcError):
+            f()
+
+
 def test_captured_and_on_another_stream(ic):
     """Write, attention and weights captured once and replayed on new contents, beside eager work."""
     say("graph of write, attention, weights")
