@@ -961,10 +961,23 @@ __global__ __launch_bounds__(256, 1) void kv4_attn_few_kernel(Kv4AttnArgs a)
 //
 // probs[q, slot] = 1/H sum_h exp(sm_scale <Q[h], K[row]> - lse[h]).  The same tiles as above with the operands exchanged:
 // heads are the matrix rows, cache rows the columns, so a lane holds 16 heads of one cache row and adds them up by itself.
+// A step multiplies one tile and, between its products, takes the exponentials of the tile before.
+struct ProbTiles {
+    static constexpr int kSlotB = kCodeB;
+    unsigned char code[4][3][kCodeB];         // [wave][ring]
+    unsigned char q[32 * 2 * kRow];           // (four waves to a query)
+    unsigned char rope[4][kRopeB];
+    int32_t idx[4][8][kT], page[4][4][kT];
+    unsigned int scale[4][4][kT];
+    unsigned int code_at[4][4][8], rope_at[4][2][8][4];
+    float off[4][32];                         // the heads' log-sum-exps in log2 units
+    __device__ __forceinline__ unsigned char *codes(int wave) { return &code[wave][0][0]; }
+};
+
 template <int W, bool PAGED, bool WIDE>
 __global__ __launch_bounds__(256, 1) void kv4_probs_kernel(Kv4AttnArgs a)
 {
-    __shared__ __attribute__((aligned(1024))) Tiles lds;
+    __shared__ __attribute__((aligned(1024))) ProbTiles lds;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, g = lane >> 5;
     const int nq = a.B * a.Tq;
@@ -972,15 +985,20 @@ __global__ __launch_bounds__(256, 1) void kv4_probs_kernel(Kv4AttnArgs a)
     const int q0 = W > 1 ? wg / a.n_splits : (wgs & 7) == 0 ? ((wg & 7) * (wgs >> 3) + (wg >> 3)) * 4 + wave : wg * 4 + wave;
     const int split = W > 1 ? wg - q0 * a.n_splits : 0;
     if (W == 1 && q0 >= nq) return;
-    Fetch<W, PAGED, WIDE, Tiles> f(a, lds, wave, q0, wgs * 4, split, W == 1 ? 0 : wave);
-    unsigned int n = 0, ok[3];
+    Fetch<W, PAGED, WIDE, ProbTiles> f(a, lds, wave, q0, wgs * 4, split, W == 1 ? 0 : wave);
+    if (W > 1) ask_q(a, q0, (unsigned)__builtin_amdgcn_readfirstlane((int)lds_offset(lds.q)), wave, lane);
+    unsigned int n = 0, slot = 0, ok[3];
     f.begin(lane, ok);
+    if (W > 1) meet();
     const float inv_h = 1.f / (float)a.H_q;
+    const int gr = 16 * (g ^ (l32 & 15)), rr = 16 * (g ^ (l32 >> 1 & 7));
+    auto k_at = [&](unsigned int at) __attribute__((always_inline)) { return &lds.code[wave][at][l32 * 256]; };
 #pragma unroll 1
   for (int q = q0; q < nq; q += f.stride) {
     bf16x8 ql[8][4], qr[4];
-    float off[16];                              // of head 8 (i / 4) + 4 g + i % 4, log2 units
-    {
+    if (W > 1) {
+        read_q(lds.q, lane, ql, qr);
+    } else {
         const unsigned short *qp = (const unsigned short *)a.Q + ((int64_t)q * a.H_q + (l32 < a.H_q ? l32 : 0)) * kRow;
 #pragma unroll
         for (int j = 0; j < 8; ++j)
@@ -989,56 +1007,112 @@ __global__ __launch_bounds__(256, 1) void kv4_probs_kernel(Kv4AttnArgs a)
                 ql[j][s] = *(const bf16x8 *)(qp + 64 * j + 32 * g + 8 * s);
 #pragma unroll
         for (int r = 0; r < 4; ++r) qr[r] = *(const bf16x8 *)(qp + kLat + 16 * r + 8 * g);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int h = 8 * (i >> 2) + 4 * g + (i & 3);
-            const float x = a.lse[(int64_t)q * a.H_q + min(h, a.H_q - 1)];
-            off[i] = h < a.H_q ? x * 1.4426950408889634f : INFINITY;
-        }
     }
+    // (heads that are not there: nothing is left of exp2(s - inf))
+    lds.off[wave][l32] = l32 < a.H_q ? a.lse[(int64_t)q * a.H_q + l32] * 1.4426950408889634f : INFINITY;
+    float z[16];                                // of the tile before: log2 of the probabilities of heads 8 (i / 4) + 4 g + i % 4
+    unsigned int have = 0;
+    int at = -1;                                // its slot of this lane
+    auto pin = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) asm volatile("" : "+v"(ql[j][0]), "+v"(ql[j][1]), "+v"(ql[j][2]), "+v"(ql[j][3]));
-    asm volatile("" : "+v"(qr[0]), "+v"(qr[1]), "+v"(qr[2]), "+v"(qr[3]));
+        for (int j = 0; j < 8; ++j) asm volatile("" : "+v"(ql[j][0]), "+v"(ql[j][1]), "+v"(ql[j][2]), "+v"(ql[j][3]));
+        asm volatile("" : "+v"(qr[0]), "+v"(qr[1]), "+v"(qr[2]), "+v"(qr[3]));
+    };
+    pin();
+    auto write = [&](float p) __attribute__((always_inline)) {
+        p = half_sum(p);
+        if (g == 0 && (unsigned)at < (unsigned)f.n_slots) a.probs[(int64_t)q * a.k_sel + f.s0 + at] = (have >> l32) & 1u ? p * inv_h : 0.f;
+    };
+    auto finish = [&]() __attribute__((always_inline)) {
+        float p = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) asm volatile("" : "+v"(off[i]));
+        for (int i = 0; i < 16; ++i) p += __builtin_amdgcn_exp2f(z[i]);
+        write(p);
+    };
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z[i] = 0.f;
+    u32x4 kc[3];                               // K's codes, chunks j in [j % 3]; of the tile that comes 0 and 1, and its exponents
+    kc[0] = *(const u32x4 *)(k_at(slot) + gr);
+    kc[1] = *(const u32x4 *)(k_at(slot) + (32 ^ gr));
+    unsigned int sc = lds.scale[wave][n & 3][l32];
 #pragma unroll 1
     for (int t = f.first; t < f.n_tiles; t += W, ++n) {
-        f.ask_codes(f.code_slot(n + 2), lane);
-        f.ask_pages(n + 4, f.entry(n + 4, lane));
-        f.ask_ids(n + 6, lane);
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kAhead) : "memory");
-        const unsigned char *kp = &lds.code[wave][0][0] + (n & (kRing - 1)) * kCodeB + l32 * 256;
-        const unsigned int sc = lds.scale[wave][n & 3][l32];
-        f32x16 s;
+        pin();
+        const unsigned int two = slot == 0 ? 2 : slot - 1;
+        const unsigned int to = f.code0 + two * kCodeB;
+        if (ok[0] == 0u) {
+            f.ask_codes(to, lane);
+            f.ask_pages(n + 4, f.entry(n + 4, lane));
+            f.ask_ids(n + 6, lane);
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kAhead) : "memory");
+            finish();
+            // (what is written for this tile is zero, whatever z holds)
+        } else {
+            const unsigned char *const krow = k_at(slot), *const rrow = &lds.rope[wave][l32 * 128];
+            f32x16 s;
+            bf16x8 kb[3], rk[3];
+            float sf[4], p = 0.f;
+            f32x4 off[4];
+            u32x4 cr;
+            int pe = 0;
+            const unsigned int piece = f.code_piece(lane);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+            for (int j = 0; j < 4; ++j) sf[j] = scale_of((sc >> (8 * j)) & 255u);
+            kb[0] = widen(kc[0][0], sf[0]);
+            kb[1] = widen(kc[0][1], sf[0]);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const bf16x8 k = *(const bf16x8 *)(&lds.rope[wave][0] + l32 * 128 + (((2 * r + g) ^ (l32 >> 1 & 7)) << 4));
-            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qr[r], k, s, 0, 0, 0);
+            for (int i = 0; i < 32; ++i) {
+                const int j = i >> 2, e = i & 3;
+                if (i == 0)
+                    mfma_new(s, ql[0][0], kb[0]);
+                else
+                    mfma_add(s, ql[j][e], kb[i % 3]);
+                __builtin_amdgcn_sched_barrier(0);
+                if (i < 30) kb[(i + 2) % 3] = widen(kc[((i + 2) >> 2) % 3][(i + 2) & 3], sf[(i + 2) >> 3]);
+                if (e == 0 && j < 6) kc[(j + 2) % 3] = *(const u32x4 *)(krow + ((32 * (j + 2)) ^ gr));
+                if (i == 1 || i == 11) cr = f.code_rows(i > 1, lane);
+                if (i == 6) f.template ask_code<0>(to, cr[0], piece);
+                if (i == 7) f.template ask_code<1>(to, cr[1], piece);
+                if (i == 8) f.template ask_code<2>(to, cr[2], piece);
+                if (i == 9) f.template ask_code<3>(to, cr[3], piece);
+                if (i == 16) f.template ask_code<4>(to, cr[0], piece);
+                if (i == 17) f.template ask_code<5>(to, cr[1], piece);
+                if (i == 18) f.template ask_code<6>(to, cr[2], piece);
+                if (i == 19) f.template ask_code<7>(to, cr[3], piece);
+                if (PAGED && i == 13) pe = f.entry(n + 4, lane);
+                if (i == 20) f.ask_pages(n + 4, pe);
+                if (i == 21) f.ask_ids(n + 6, lane);
+                if (i == 22) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kAhead) : "memory");
+                if (i >= 23 && i < 26) rk[i - 23] = *(const bf16x8 *)(rrow + ((32 * (i - 23)) ^ rr));
+                if (i >= 2 && i < 18) p += __builtin_amdgcn_exp2f(z[i - 2]);
+                if (i >= 26 && i < 30) off[i - 26] = *(const f32x4 *)&lds.off[wave][8 * (i - 26) + 4 * g];
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                mfma_add(s, qr[r], rk[r % 3]);
+                __builtin_amdgcn_sched_barrier(0);
+                if (r == 0) rk[0] = *(const bf16x8 *)(rrow + (96 ^ rr));
+                if (r == 1) write(p);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            mfma_settle(s);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[i] = __builtin_fmaf(s[i], a.scale_log2e, -off[i >> 2][i & 3]);
         }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        have = ok[0];
+        at = t * kT + l32;
         f.ask_ropes(n + 1, lane);
-        const unsigned int have = ok[0];
         ok[0] = ok[1];
         ok[1] = ok[2];
         ok[2] = f.find_rows(n + 3, f.entry(n + 3, lane), f.page(n + 3, lane), lane);
         f.advance();
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const u32x4 c = *(const u32x4 *)(kp + (((2 * j + g) ^ (l32 & 15)) << 4));
-            const float x = scale_of((sc >> (8 * (j >> 1))) & 255u);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ql[j][e], widen(c[e], x), s, 0, 0, 0);
-        }
-        float p = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-            if (off[i] != INFINITY) p += __builtin_amdgcn_exp2f(s[i] * a.scale_log2e - off[i]);
-        p = half_sum(p);
-        const int at = t * kT + l32;
-        if (g == 0 && at < f.n_slots) a.probs[(int64_t)q * a.k_sel + f.s0 + at] = (have >> l32) & 1u ? p * inv_h : 0.f;
+        slot = slot == 2 ? 0 : slot + 1;
+        kc[0] = *(const u32x4 *)(k_at(slot) + gr);
+        kc[1] = *(const u32x4 *)(k_at(slot) + (32 ^ gr));
+        sc = lds.scale[wave][(n + 1) & 3][l32];
     }
+    finish();
     if (W > 1) break;
   }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
