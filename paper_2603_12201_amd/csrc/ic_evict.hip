@@ -27,44 +27,84 @@ __device__ __forceinline__ unsigned long long fixed48(float p)
 
 constexpr int kWeightThreads = 1024;
 constexpr int kMaxRange = 16384;              // positions of a range: 128 KB of LDS
+constexpr int kFewRange = 4096;               // of a range when there are few entries (weight_plan())
 constexpr int kMaxChunkRows = 1 << 15;        // rows whose sum fits 64 bits: 2^15 2^48
 
+template <int RANGE>
 __global__ __launch_bounds__(kWeightThreads) void weight_kernel(WeightArgs a)
 {
-    __shared__ unsigned long long sum[kMaxRange];
+    __shared__ unsigned long long sum[RANGE];
     const int tid = threadIdx.x;
     const int range = blockIdx.x % a.n_ranges, rest = blockIdx.x / a.n_ranges;
     const int chunk = rest % a.n_chunks, b = rest / a.n_chunks;
     const int lo = range * a.range, n = min(a.range, a.Lk - lo);
-    for (int i = tid; i < n; i += kWeightThreads) sum[i] = 0ull;
-    __syncthreads();
     const int64_t t0 = (int64_t)chunk * a.chunk_rows, t1 = min(t0 + a.chunk_rows, (int64_t)a.Tq);
     const int64_t at = ((int64_t)b * a.Tq + t0) * a.k_sel, entries = (t1 - t0) * a.k_sel;
     const int32_t *idx = a.idx + at;
     const float *p = a.probs + at;
-    for (int64_t e = tid; e < entries; e += kWeightThreads) {
-        const int s = idx[e] - lo;
-        if (s >= 0 && s < n) atomicAdd(&sum[s], fixed48(p[e]));
+    const int64_t w0 = (int64_t)b * a.Lk + lo;
+    // what was there, asked for ahead of everything (4096 positions: 4 a thread)
+    float in[kFewRange / kWeightThreads];
+    if (RANGE == kFewRange && a.n_chunks == 1 && a.in)
+#pragma unroll
+        for (int j = 0; j < kFewRange / kWeightThreads; ++j) in[j] = a.in[w0 + min(j * kWeightThreads + tid, n - 1)];
+    for (int i = tid; i < n; i += kWeightThreads) sum[i] = 0ull;
+    __syncthreads();
+    // eight entries a thread at a time: one after the other, their loads take as long as everything else (67 us against 26 for 8191 rows of 2048)
+    constexpr int kAtOnce = 8;
+    for (int64_t e0 = 0; e0 < entries; e0 += kAtOnce * kWeightThreads) {
+        const int32_t *const ie = idx + e0;
+        const float *const pe = p + e0;
+        const int left = (int)min((int64_t)kAtOnce * kWeightThreads, entries - e0);
+        int s[kAtOnce];
+        float v[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int e = u * kWeightThreads + tid;
+            s[u] = ie[min(e, left - 1)] - lo;
+            s[u] = e < left && s[u] >= 0 && s[u] < n ? s[u] : -1;
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) v[u] = pe[s[u] >= 0 ? u * kWeightThreads + tid : 0];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u)
+            if (s[u] >= 0) atomicAdd(&sum[s[u]], fixed48(v[u]));
     }
     __syncthreads();
-    for (int i = tid; i < n; i += kWeightThreads) {
-        if (a.n_chunks == 1) {
-            const int64_t w = (int64_t)b * a.Lk + lo + i;
-            a.out[w] = (float)((a.in ? (double)a.in[w] : 0.0) + (double)sum[i] * 0x1p-48);
-        } else {
-            a.part[((int64_t)b * a.n_chunks + chunk) * a.Lk + lo + i] = sum[i];
+    if (a.n_chunks > 1) {
+        unsigned long long *const part = a.part + (((int64_t)b * a.n_chunks + chunk) * a.Lk + lo);
+        for (int i = tid; i < n; i += kWeightThreads) part[i] = sum[i];
+    } else if (RANGE == kFewRange) {
+#pragma unroll
+        for (int j = 0; j < kFewRange / kWeightThreads; ++j) {
+            const int i = j * kWeightThreads + tid;
+            if (i < n) a.out[w0 + i] = (float)((a.in ? (double)in[j] : 0.0) + (double)sum[i] * 0x1p-48);
         }
+    } else {
+        for (int i = tid; i < n; i += kWeightThreads) a.out[w0 + i] = (float)((a.in ? (double)a.in[w0 + i] : 0.0) + (double)sum[i] * 0x1p-48);
     }
 }
 
-__global__ __launch_bounds__(256) void weight_sum_kernel(WeightArgs a)
+// The chunks' sums: 32 positions a workgroup, 32 threads to each, whose sums are added in their order.
+__global__ __launch_bounds__(1024) void weight_sum_kernel(WeightArgs a)
 {
-    const int64_t w = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (w >= (int64_t)a.B * a.Lk) return;
-    const int64_t b = w / a.Lk, s = w - b * a.Lk;
-    double t = a.in ? (double)a.in[w] : 0.0;
-    for (int c = 0; c < a.n_chunks; ++c) t += (double)a.part[(b * a.n_chunks + c) * a.Lk + s] * 0x1p-48;
-    a.out[w] = (float)t;
+    __shared__ double sums[32][33];
+    const int tid = threadIdx.x, x = tid & 31, y = tid >> 5;
+    const int64_t w0 = (int64_t)blockIdx.x * 32, all = (int64_t)a.B * a.Lk, w = w0 + x;
+    if (w < all) {
+        const int64_t b = w / a.Lk;
+        const unsigned long long *const part = a.part + (b * a.n_chunks * a.Lk + (w - b * a.Lk));
+        double t = 0.0;
+#pragma unroll 4
+        for (int c = y; c < a.n_chunks; c += 32) t += (double)part[(int64_t)c * a.Lk] * 0x1p-48;
+        sums[y][x] = t;
+    }
+    __syncthreads();
+    if (y == 0 && w < all) {
+        double t = a.in ? (double)a.in[w] : 0.0;
+        for (int c = 0; c < 32; ++c) t += sums[c][x];
+        a.out[w] = (float)t;
+    }
 }
 
 // Order of the weights as unsigned integers (-0 and +0 are one value, a NaN is above infinity).
@@ -387,9 +427,13 @@ __global__ __launch_bounds__(256) void compact_kernel(CompactArgs a)
 } // namespace
 
 // Ranges and chunks of a call.  One chunk: the launch writes the weights itself.
+// A range is what LDS holds, as every range's workgroup goes through all of the entries; with no more than two of them per
+// position of a short range the positions cost more, and four times the workgroups take them (32 sequences of 65536 positions,
+// 2048 entries each: 7.8 us against 11.5).
 void weight_plan(WeightArgs &a)
 {
-    a.range = a.Lk < kMaxRange ? a.Lk : kMaxRange;
+    const int most = (int64_t)a.Tq * a.k_sel <= 2 * kFewRange ? kFewRange : kMaxRange;
+    a.range = a.Lk < most ? a.Lk : most;
     a.n_ranges = (a.Lk + a.range - 1) / a.range;
     int chunks = 1;
     if (a.Tq > 16) {
@@ -404,11 +448,15 @@ void weight_plan(WeightArgs &a)
 
 hipError_t launch_weight_add(const WeightArgs &a, hipStream_t st)
 {
-    hipLaunchKernelGGL(weight_kernel, dim3((unsigned)(a.B * a.n_ranges * a.n_chunks)), dim3(kWeightThreads), 0, st, a);
+    const dim3 grid((unsigned)(a.B * a.n_ranges * a.n_chunks)), block(kWeightThreads);
+    if (a.range <= kFewRange)
+        hipLaunchKernelGGL((weight_kernel<kFewRange>), grid, block, 0, st, a);
+    else
+        hipLaunchKernelGGL((weight_kernel<kMaxRange>), grid, block, 0, st, a);
     if (a.n_chunks > 1) {
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        hipLaunchKernelGGL(weight_sum_kernel, dim3((unsigned)(((int64_t)a.B * a.Lk + 255) / 256)), dim3(256), 0, st, a);
+        hipLaunchKernelGGL(weight_sum_kernel, dim3((unsigned)(((int64_t)a.B * a.Lk + 31) / 32)), dim3(1024), 0, st, a);
     }
     return hipGetLastError();
 }
