@@ -1742,7 +1742,9 @@ ic_status ic_attn_probs_kv4(const ic_attn_desc *d, const ic_paged_cache *pc, int
     const Kv4Splits sp = kv4_splits(d);
     a.n_splits = sp.n;
     a.split_len = sp.len;
-    hipError_t e = ic::launch_kv4_probs(a, (int64_t)d->B * d->Tq < 1024, (hipStream_t)stream);
+    // (2048 rows each, 768 queries of a sequence each: 140 us with four waves to a query, 156 with one; of one sequence 69 and 77;
+    // 1000 queries: 180 and 180, 90 and 80)
+    hipError_t e = ic::launch_kv4_probs(a, (int64_t)d->B * d->Tq <= 768, (hipStream_t)stream);
     if (e != hipSuccess) return fail(IC_ERR_HIP, "4-bit attention-probability launch failed: %s", hipGetErrorString(e));
     return IC_OK;
 }
