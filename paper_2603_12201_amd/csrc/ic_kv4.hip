@@ -226,8 +226,7 @@ __device__ __forceinline__ void to_lds4(const void *base, unsigned int off, unsi
 // the codes of tile n + 2 (8 instructions), the page numbers of n + 4, the entries of idx of n + 6, a wait for all but these 10
 // and the one before them, and when tile n's rotary part has been read that of n + 1 (4) and the exponents of n + 3.  Nothing of
 // it passes through registers, loads return in order, and nothing else loads within the loop over a query's tiles: behind the
-// wait, everything that earlier steps have asked for but their last has arrived.
-constexpr int kAhead = 11;
+// wait, everything that earlier steps have asked for but their last has arrived.  (Without a page table nothing asks for page numbers.)
 struct Cursor {
     int q;                                    // query row; n_queries and more: none
     int tile, b, len;                         // len: 0 where there is no such query
@@ -236,6 +235,7 @@ struct Cursor {
 // W waves share a query: each takes every W-th tile.  WIDE: rows behind 4 GB, in the 32-bit offsets of the others they are not.
 template <int W, bool PAGED, bool WIDE, typename LDS>
 struct Fetch {
+    static constexpr int kAhead = 10 + PAGED; // what may be on its way behind the wait
     const Kv4AttnArgs &a;
     LDS &lds;
     unsigned int code0, rope0, idx0, page0, scale0;   // LDS addresses of this wave's
@@ -297,9 +297,7 @@ struct Fetch {
     __device__ __forceinline__ int page(unsigned int m, int lane) const { return PAGED ? lds.page[wave][m & 3][lane & 31] : 0; }
     __device__ __forceinline__ void ask_pages(unsigned int m, int s) const        // s: entry() of tile m
     {
-        if (!PAGED)
-            to_lds4(a.idx, 0u, page0 + (m & 3) * (kT * 4));                 // (any word: the number of loads is the same)
-        else
+        if (PAGED)
             to_lds4(a.pv.page_table + (int64_t)pages.b * a.pv.max_pages, (unsigned)s < (unsigned)pages.len ? 4u * (unsigned)(s >> a.pv.page_shift) : 0u,
                     page0 + (m & 3) * (kT * 4));
     }
@@ -373,12 +371,14 @@ struct Fetch {
             next_ids();
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if (PAGED) {
 #pragma unroll 1
-        for (unsigned int i = 0; i < 4; ++i) {
-            ask_pages(i, entry(i, lane));
-            next(pages);
+            for (unsigned int i = 0; i < 4; ++i) {
+                ask_pages(i, entry(i, lane));
+                next(pages);
+            }
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
         for (unsigned int i = 0; i < 3; ++i) {
             ok[i] = find_rows(i, entry(i, lane), page(i, lane), lane);
@@ -558,7 +558,7 @@ __global__ __launch_bounds__(256, 1) void kv4_attn_kernel(Kv4AttnArgs a)
             f.ask_codes(f.code_slot(n + 2), ln);
             f.ask_pages(n + 4, f.entry(n + 4, ln));
             f.ask_ids(n + 6, ln);
-            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kAhead) : "memory");
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(f.kAhead) : "memory");
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = -INFINITY;
             am = amounts(m1, 0, g);
@@ -608,7 +608,7 @@ __global__ __launch_bounds__(256, 1) void kv4_attn_kernel(Kv4AttnArgs a)
                 if (PAGED && i == 13) pe = f.entry(n + 4, ln);
                 if (i == 20) f.ask_pages(n + 4, pe);
                 if (i == 21) f.ask_ids(n + 6, ln);
-                if (i == 22) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kAhead) : "memory");
+                if (i == 22) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(f.kAhead) : "memory");
                 if (i == 12) am = amounts(m1, 0, g);
                 if (i >= 23 && i < 26) rk[i - 23] = rope_piece(i - 23);
                 if (i >= 26 && i < 30) {
@@ -813,7 +813,7 @@ __global__ __launch_bounds__(256, 1) void kv4_attn_few_kernel(Kv4AttnArgs a)
         if (ok[0] == 0u) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = -INFINITY;
-            asm volatile("s_waitcnt vmcnt(11)" ::: "memory");
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(f.kAhead) : "memory");
         } else {
             const unsigned char *const krow = k_at(slot), *const rrow = &lds.rope[wave][kr * 128];
             bf16x8 kb[3], rk[3];
@@ -834,7 +834,7 @@ __global__ __launch_bounds__(256, 1) void kv4_attn_few_kernel(Kv4AttnArgs a)
                 if (e == 0 && j < 6) kc[(j + 2) % 3] = *(const u32x4 *)(krow + ((32 * (j + 2)) ^ gr));
                 if (i >= 2 && i < 6)
                     lds.amount[n & 1][wave][i - 2][(l32 >> 2) & 1][4 * (l32 >> 3) + (l32 & 3)] = (unsigned short)(kAmount - (int)(((sc >> (8 * (i - 2))) & 255u) << 7));
-                if (i == 25) asm volatile("s_waitcnt vmcnt(11)" ::: "memory");  // (what was asked for behind the rotary part)
+                if (i == 25) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(f.kAhead) : "memory");  // (what was asked for behind the rotary part)
                 if (i >= 26 && i < 29) rk[i - 26] = *(const bf16x8 *)(rrow + ((32 * (i - 26)) ^ rr));
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -887,7 +887,7 @@ __global__ __launch_bounds__(256, 1) void kv4_attn_few_kernel(Kv4AttnArgs a)
         lds.p[n & 1][wave][1][lane] = p[1];
         ok[0] = ok[1];
         ok[1] = ok[2];
-        asm volatile("s_waitcnt vmcnt(14)" ::: "memory");                   // (this step's: the page numbers of n + 3 were asked for a step ago)
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(f.kAhead + 3) : "memory");  // (this step's: the page numbers of n + 3 were asked for a step ago)
         ok[2] = f.find_rows(n + 3, f.entry(n + 3, lane), f.page(n + 3, lane), lane);
         f.advance();
         meet();
@@ -1058,7 +1058,7 @@ __global__ __launch_bounds__(256, 1) void kv4_probs_kernel(Kv4AttnArgs a)
             f.ask_codes(to, lane);
             f.ask_pages(n + 4, f.entry(n + 4, lane));
             f.ask_ids(n + 6, lane);
-            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kAhead) : "memory");
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(f.kAhead) : "memory");
             finish();
             // (what is written for this tile is zero, whatever its z)
 #pragma unroll
@@ -1100,7 +1100,7 @@ __global__ __launch_bounds__(256, 1) void kv4_probs_kernel(Kv4AttnArgs a)
                 if (PAGED && i == 13) pe = f.entry(n + 4, lane);
                 if (i == 20) f.ask_pages(n + 4, pe);
                 if (i == 21) f.ask_ids(n + 6, lane);
-                if (i == 22) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kAhead) : "memory");
+                if (i == 22) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(f.kAhead) : "memory");
                 if (i >= 23 && i < 26) rk[i - 23] = *(const bf16x8 *)(rrow + ((32 * (i - 23)) ^ rr));
                 if (i >= 2 && i < 18) p += __builtin_amdgcn_exp2f(z[i - 2]);
                 if (i == 14) e3 = f.entry(n + 3, lane);
