@@ -297,7 +297,7 @@ ic_status ic_attn_probs_kv4(const ic_attn_desc *desc, const ic_paged_cache *pc, 
  *   probs, idx [B,Tq,k_sel] as ic_attn_probs and ic_indexer_topk leave them (entries outside [0, Lk) are skipped, equal
  *   entries of a row all count); weight_in [B,Lk] fp32, nullable (zeros), may be weight itself; weight [B,Lk] fp32 out.
  *   A probability below 0 or not a number counts as 0, one above 1 as 1; each is taken to 2^-48, and their sum is the same
- *   whatever the order.  workspace: ic_attn_weight_add_workspace() bytes (0 for a few rows).
+ *   whatever the order (a row's probabilities at one position must add up to less than 2).  workspace: ic_attn_weight_add_workspace() bytes (0 for a few rows).
  *
  * ic_evict_keep: the positions of each sequence that stay when at most n_keep do.  A sequence of n = min(Lk, seq_lens[b])
  *   positions (seq_lens NULL: Lk) keeps all if n <= n_keep; otherwise the first n_first, the last n_recent, and of the
@@ -311,8 +311,8 @@ ic_status ic_attn_probs_kv4(const ic_attn_desc *desc, const ic_paged_cache *pc, 
  *   multiple of 4 bytes) to their new positions: row keep[b][j] of sequence b becomes row j.  src: [B,Lk,row_bytes], or the
  *   pool of src_pc's page table; dst: [B,n_keep,row_bytes], or the pool of dst_pc's (which covers n_keep positions).  The
  *   seq_lens of both are ignored.  Rows behind a sequence's last kept one stay as they were, as does the rest of a pool.  The
- *   rows written must be none of the rows read: src and dst ranges may not meet, except as one pool with different page
- *   tables whose pages differ.  src_rows, dst_rows: rows that the buffers hold; row numbers outside them are left out.
+ *   rows written must be none of the rows read: no dst range may meet a src range or another dst, except a cache's own as one
+ *   pool with different page tables whose pages differ.  src_rows, dst_rows: rows that the buffers hold; row numbers outside them are left out.
  */
 #define IC_MAX_MOVE_CACHES 16
 typedef struct ic_cache_move {

@@ -1862,6 +1862,11 @@ ic_status ic_cache_compact(const ic_cache_move *caches, int32_t n_caches, int32_
         const Range s = {(const char *)c.src, (size_t)c.src_rows * c.row_bytes}, d = {(const char *)c.dst, (size_t)c.dst_rows * c.row_bytes};
         const bool pages = sp && dp && c.src == c.dst && src_pc->page_table != dst_pc->page_table;
         if (s.meets(d) && !pages) return fail(IC_ERR_SHAPE, "cache %d: src and dst overlap", i);
+        for (int j = 0; j < i; ++j) {
+            const ic_cache_move &o = caches[j];
+            const Range os = {(const char *)o.src, (size_t)o.src_rows * o.row_bytes}, od = {(const char *)o.dst, (size_t)o.dst_rows * o.row_bytes};
+            if (d.meets(os) || d.meets(od) || s.meets(od)) return fail(IC_ERR_SHAPE, "caches %d and %d: what one writes overlaps the other", j, i);
+        }
         a.src[i] = (const unsigned char *)c.src;
         a.dst[i] = (unsigned char *)c.dst;
         a.row_bytes[i] = c.row_bytes;

@@ -123,6 +123,23 @@ def test_weights_and_eviction_are_checked(ic):
     assert move(src=4096, dst=4096, sp=same, dp=same) == S.ERR_SHAPE             # rows onto themselves
 
 
+def test_caches_of_one_call_must_not_write_over_each_other(ic):
+    """Two moves of 100 rows to 50 of 400 bytes each, at addresses that nothing reads before the refusal."""
+    S, L = ic.Status, ic.lib()
+    far = 1 << 20
+
+    def move(src0, dst0, src1, dst1):
+        m = (ic.CacheMove * 2)()
+        for c, (src, dst) in zip(m, ((src0, dst0), (src1, dst1))):
+            c.src, c.dst, c.src_rows, c.dst_rows, c.row_bytes, c.reserved = src, dst, 100, 50, 400, 0
+        return L.ic_cache_compact(m, 2, 1, 100, 50, C.c_void_p(4096), None, None, None)
+
+    assert move(far, 2 * far, 3 * far, 2 * far) == S.ERR_SHAPE                   # one destination twice
+    assert move(far, 2 * far, 3 * far, 2 * far + 19996) == S.ERR_SHAPE           # its last row
+    assert move(far, 2 * far, 3 * far, far + 4000) == S.ERR_SHAPE                # the second writes what the first reads
+    assert move(far, 2 * far, 2 * far + 8000, 4 * far) == S.ERR_SHAPE            # the second reads what the first writes
+
+
 def test_binding_refuses_what_it_can_see(ic):
     import torch
     t = torch.zeros((1, 4, 576), dtype=torch.bfloat16)
