@@ -1857,7 +1857,7 @@ ic_status ic_cache_compact(const ic_cache_move *caches, int32_t n_caches, int32_
         if (c.reserved != 0) return fail(IC_ERR_UNSUPPORTED, "reserved must be 0");
         if (c.row_bytes <= 0 || c.row_bytes % 4 != 0 || c.row_bytes > (1 << 20) || !aligned(c.src, 4) || !aligned(c.dst, 4))
             return fail(IC_ERR_SHAPE, "cache %d: rows of %d bytes (a multiple of 4, 4-byte aligned)", i, c.row_bytes);
-        if (c.src_rows <= 0 || c.dst_rows <= 0 || (!sp && c.src_rows < (int64_t)B * Lk) || (!dp && c.dst_rows < (int64_t)B * n_keep))
+        if (c.src_rows <= 0 || c.dst_rows <= 0 || c.src_rows > (int64_t)1 << 40 || c.dst_rows > (int64_t)1 << 40 || (!sp && c.src_rows < (int64_t)B * Lk) || (!dp && c.dst_rows < (int64_t)B * n_keep))
             return fail(IC_ERR_SHAPE, "cache %d: src_rows=%lld dst_rows=%lld do not hold the sequences", i, (long long)c.src_rows, (long long)c.dst_rows);
         const Range s = {(const char *)c.src, (size_t)c.src_rows * c.row_bytes}, d = {(const char *)c.dst, (size_t)c.dst_rows * c.row_bytes};
         const bool pages = sp && dp && c.src == c.dst && src_pc->page_table != dst_pc->page_table;

@@ -226,6 +226,8 @@ CASES = [
     (2, 600, 640, 9, 100, 64, False, True),       # a wave per query, 1200 of them
     (1, 1030, 1030, 32, 257, 0, False, False),    # the same, causal rows, a last workgroup of two waves
     (1, 3, 400, 32, 2500, 0, False, False),       # more slots than keys
+    (1, 256, 300, 31, 96, 128, True, False),      # a workgroup per query, three of its four waves with a tile
+    (3, 171, 400, 32, 130, 64, True, True),       # 513 queries: the weights still four waves to a query, the attention one
 ]
 
 
