@@ -168,14 +168,14 @@ def _check(rc):
 
 
 def _ptr(t):
-    return None if t is None else C.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
 def _stream(stream):
     import torch
     if stream is None:                                     # (torch.cuda.current_stream() without its object: 0.3 us, not 3)
-        return C.c_void_p(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
-    return C.c_void_p(stream.cuda_stream)
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    return stream.cuda_stream
 
 
 def _dtype_code(t):
@@ -576,13 +576,12 @@ def _current_device():
     return torch._C._cuda_getDevice()
 
 
-def _same_device(like, **tensors):
+def _same_device(*tensors):
     """All on one device, and that the current one, whose stream the kernels go to."""
-    if like.device.index != _current_device():
-        raise IcError(Status.ERR_SHAPE, "the tensors are on %s, which is not the current device" % like.device)
-    for name, t in tensors.items():
-        if t is not None and t.device != like.device:
-            raise IcError(Status.ERR_SHAPE, "%s is on %s, not on %s" % (name, t.device, like.device))
+    here = _current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise IcError(Status.ERR_SHAPE, "a tensor %s is on %s, the current device is %d" % (tuple(t.shape), t.device, here))
 
 
 def _kv4_cache(kv4, B, Lk, pc):
@@ -596,7 +595,7 @@ def _kv4_cache(kv4, B, Lk, pc):
         lens, table = pc._keep
         if (lens is not None and lens.shape[0] != B) or (table is not None and table.shape[0] != B):
             raise IcError(Status.ERR_SHAPE, "seq_lens / page_table are not for %d sequences" % B)
-        _same_device(kv4, seq_lens=lens, page_table=table)
+        _same_device(lens, table)
     if not paged and (kv4.dim() != 3 or kv4.shape[0] != B):
         raise IcError(Status.ERR_SHAPE, "kv4 %s must be [%d, Lk, %d] without a page table" % (tuple(kv4.shape), B, KV4_ROW_BYTES))
     if Lk is None:
@@ -621,7 +620,7 @@ def kv4_write(rows, kv4, pos0=0, Lk=None, pc=None, stream=None):
     if width != 576:
         raise IcError(Status.ERR_UNSUPPORTED, "rows of %d elements (576)" % width)
     Lk, n = _kv4_cache(kv4, B, Lk, pc)
-    _same_device(kv4, rows=rows)
+    _same_device(kv4, rows)
     d = Kv4Desc(B, Tn, Lk, 0, pos0, n)
     _check(lib().ic_kv4_write(C.byref(d), _ref(pc), _ptr(rows), _ptr(kv4), _stream(stream)))
     return kv4
@@ -637,7 +636,7 @@ def kv4_read(kv4, B, Tn, pos0=0, Lk=None, pc=None, stream=None, out=None):
     _need(out, "out", torch.bfloat16, 3)
     if tuple(out.shape) != (B, Tn, 576):
         raise IcError(Status.ERR_SHAPE, "out %s must be %s" % (tuple(out.shape), (B, Tn, 576)))
-    _same_device(kv4, out=out)
+    _same_device(kv4, out)
     d = Kv4Desc(B, Tn, Lk, 0, pos0, n)
     _check(lib().ic_kv4_read(C.byref(d), _ref(pc), _ptr(kv4), _ptr(out), _stream(stream)))
     return out
@@ -651,7 +650,6 @@ def _kv4_attn_desc(Q, kv4, idx, sm_scale, Lk, pc):
     if idx.shape[0] != B or idx.shape[1] != Tq:
         raise IcError(Status.ERR_SHAPE, "Q %s and idx %s disagree" % (tuple(Q.shape), tuple(idx.shape)))
     Lk, n = _kv4_cache(kv4, B, Lk, pc)
-    _same_device(kv4, Q=Q, idx=idx)
     return AttnDesc(B, Tq, Lk, Hq, d_qk, 512, 0, 576, idx.shape[2], sm_scale), n
 
 
@@ -668,7 +666,7 @@ def sparse_attn_kv4(Q, kv4, idx, sm_scale, Lk=None, pc=None, want_lse=False, wor
         _need(O, "out", torch.bfloat16, 4)
         if tuple(O.shape) != (d.B, d.Tq, d.H_q, 512):
             raise IcError(Status.ERR_SHAPE, "out %s must be %s" % (tuple(O.shape), (d.B, d.Tq, d.H_q, 512)))
-    _same_device(kv4, out=O, workspace=workspace)
+    _same_device(kv4, Q, idx, O, workspace)
     _check(lib().ic_sparse_attn_kv4(C.byref(d), _ref(pc), n, _ptr(Q), _ptr(kv4), _ptr(idx), _ptr(O), _ptr(lse), _ptr(workspace),
                                     workspace.numel() * workspace.element_size(), _stream(stream)))
     return (O, lse) if want_lse else O
@@ -682,7 +680,7 @@ def attn_probs_kv4(Q, kv4, idx, sm_scale, lse, Lk=None, pc=None, stream=None):
     _need(lse, "lse", torch.float32, 3)
     if tuple(lse.shape) != (d.B, d.Tq, d.H_q):
         raise IcError(Status.ERR_SHAPE, "lse %s must be %s" % (tuple(lse.shape), (d.B, d.Tq, d.H_q)))
-    _same_device(kv4, lse=lse)
+    _same_device(kv4, Q, idx, lse)
     with _on(stream):
         probs = lse.new_empty(idx.shape)
     _check(lib().ic_attn_probs_kv4(C.byref(d), _ref(pc), n, _ptr(Q), _ptr(kv4), _ptr(idx), _ptr(lse), _ptr(probs), _stream(stream)))
@@ -701,7 +699,7 @@ def attn_weight_add(probs, idx, weight, out=None, workspace=None, stream=None):
     B, Tq, k = probs.shape
     if tuple(idx.shape) != (B, Tq, k) or weight.shape[0] != B or out.shape != weight.shape:
         raise IcError(Status.ERR_SHAPE, "probs %s, idx %s, weight %s, out %s disagree" % (tuple(probs.shape), tuple(idx.shape), tuple(weight.shape), tuple(out.shape)))
-    _same_device(weight, probs=probs, idx=idx, out=out, workspace=workspace)
+    _same_device(weight, probs, idx, out, workspace)
     Lk = weight.shape[1]
     if workspace is None:
         with _on(stream):
@@ -721,7 +719,7 @@ def evict_keep(weight, n_keep, n_first=0, n_recent=0, seq_lens=None, workspace=N
         _need(seq_lens, "seq_lens", torch.int32, 1)
         if seq_lens.shape[0] != B:
             raise IcError(Status.ERR_SHAPE, "seq_lens is not for %d sequences" % B)
-    _same_device(weight, seq_lens=seq_lens, workspace=workspace)
+    _same_device(weight, seq_lens, workspace)
     if n_keep <= 0:
         raise IcError(Status.ERR_SHAPE, "n_keep=%d must be positive" % n_keep)
     with _on(stream):
@@ -746,13 +744,13 @@ def cache_compact(caches, keep, Lk, src_pc=None, dst_pc=None, stream=None):
         if pc is not None and pc._keep[1] is not None:
             if pc._keep[1].shape[0] != B:
                 raise IcError(Status.ERR_SHAPE, "%s's page table is not for %d sequences" % (name, B))
-            _same_device(keep, page_table=pc._keep[1])
+            _same_device(keep, pc._keep[1])
     sp, dp = src_pc is not None and bool(src_pc.page_table), dst_pc is not None and bool(dst_pc.page_table)
     rs, rd = (1 if sp else 2), (1 if dp else 2)                                # dims in front of a row
     for m, (src, dst) in zip(moves, caches):
         _need(src, "src")
         _need(dst, "dst")
-        _same_device(keep, src=src, dst=dst)
+        _same_device(keep, src, dst)
         ss, ds = src.shape, dst.shape
         if len(ss) < rs or len(ds) < rd or src.dtype != dst.dtype or ss[rs:] != ds[rd:]:
             raise IcError(Status.ERR_SHAPE, "src %s and dst %s do not hold the same rows" % (tuple(ss), tuple(ds)))
