@@ -284,11 +284,13 @@ __global__ __launch_bounds__(kEvictThreads) void evict_kernel(EvictArgs a)
     emit_kept<R>(a, b, 0, lo, hi, len, want > 0, border, left, 0u, 0u, key, w, runs, tid);
 }
 
-// Longer sequences: a workgroup per 16384 positions and a launch per digit, and one that writes.  Each launch adds up the
-// workgroups' histograms of the digit before it (8 KB each) by itself.
-constexpr int kPartR = 16, kPart = kPartR * kEvictThreads;
+// Longer sequences: a workgroup per 8192 positions and a launch per digit, and one that writes.  Each launch adds up the
+// workgroups' histograms of the digit before it (4 KB each) by itself.  Bound by latency: weights, histograms, LDS additions one
+// after the other.  200 000 positions: 28 us in four launches (430 in one workgroup; 35 with 16384 positions and 8 KB each, 29
+// with 4096), 32 sequences of 65536 in 30.
+constexpr int kPartR = 8, kPart = kPartR * kEvictThreads;
 struct PartCounts {
-    unsigned int hist[2][2048], last[1024];
+    unsigned int hist[2][1024], last[512];    // two bins a word: a part has no more than 8192 keys
     unsigned int above[2];                    // inner keys above the border by the first digit; by the second
     unsigned int border[2], left[2];          // (of part 0: as the second and the third launch have found them)
 };
@@ -326,13 +328,13 @@ __global__ __launch_bounds__(kEvictThreads) void evict_part_kernel(EvictArgs a)
         if (bin > 0) {
 #pragma unroll 8
             for (int c = 0; c < live; ++c) {
-                const unsigned int *h = LEVEL == 3 ? seq[c].last : seq[c].hist[LEVEL - 1];
-                const u32x2 x = *(const u32x2 *)(h + bin - 1);
-                n[0] += x[1];
-                n[1] += x[0];
+                const unsigned int *h = LEVEL == 3 ? seq[c].last : seq[c].hist[(LEVEL - 1) & 1];
+                const unsigned int x = h[bin >> 1];
+                n[0] += x >> 16;
+                n[1] += x & 0xFFFFu;
                 if (LEVEL == 3 && c < part) {
-                    front[0] += x[1];
-                    front[1] += x[0];
+                    front[0] += x >> 16;
+                    front[1] += x & 0xFFFFu;
                 }
             }
         }
@@ -351,7 +353,7 @@ __global__ __launch_bounds__(kEvictThreads) void evict_part_kernel(EvictArgs a)
     if (LEVEL < 3) {
         count_digits<kPartR>(hist, key, p0, lo, hi, border, LEVEL, tid);
         unsigned int *out = LEVEL == 2 ? own->last : own->hist[LEVEL & 1];
-        for (int i = tid; i < (LEVEL == 2 ? 1024 : 2048); i += kEvictThreads) out[i] = hist[i];
+        if (tid < (LEVEL == 2 ? 512 : 1024)) out[tid] = hist[2 * tid] | hist[2 * tid + 1] << 16;
         if (LEVEL >= 1) {
             // keys above the border by the digit that this launch has found (equal in the digits before it)
             unsigned int n = 0;
