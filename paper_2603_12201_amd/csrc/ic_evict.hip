@@ -463,13 +463,19 @@ hipError_t launch_weight_add(const WeightArgs &a, hipStream_t st)
     return hipGetLastError();
 }
 
-// A workgroup holds up to 32768 keys; longer sequences are taken in parts.
-int evict_parts(int Lk) { return Lk <= 32 * kEvictThreads ? 0 : (Lk + kPart - 1) / kPart; }
-size_t evict_ws_bytes(int B, int Lk) { return (size_t)B * evict_parts(Lk) * sizeof(PartCounts); }
+// A workgroup holds up to 32768 keys, 16384 in half of the registers; longer sequences are taken in parts, from 16384 positions on
+// where the parts have a compute unit each (24000 positions: 1 sequence 20 us in parts and 29 in a workgroup, 32 22 and 29, 256
+// 49 and 33; 16384: 19 and 16, 20 and 17, 33 and 20).
+int evict_parts(int B, int Lk)
+{
+    const int parts = (Lk + kPart - 1) / kPart;
+    return Lk > 32 * kEvictThreads || (Lk > 16 * kEvictThreads && (int64_t)B * parts <= 256) ? parts : 0;
+}
+size_t evict_ws_bytes(int B, int Lk) { return (size_t)B * evict_parts(B, Lk) * sizeof(PartCounts); }
 
 hipError_t launch_evict_keep(EvictArgs a, hipStream_t st)
 {
-    a.n_parts = evict_parts(a.Lk);
+    a.n_parts = evict_parts(a.B, a.Lk);
     if (a.n_parts == 0) {
         const int per = (a.Lk + kEvictThreads - 1) / kEvictThreads;
         const dim3 grid((unsigned)a.B), block(kEvictThreads);
@@ -477,6 +483,8 @@ hipError_t launch_evict_keep(EvictArgs a, hipStream_t st)
             hipLaunchKernelGGL((evict_kernel<1>), grid, block, 0, st, a);
         else if (per <= 8)
             hipLaunchKernelGGL((evict_kernel<8>), grid, block, 0, st, a);
+        else if (per <= 16)
+            hipLaunchKernelGGL((evict_kernel<16>), grid, block, 0, st, a);
         else
             hipLaunchKernelGGL((evict_kernel<32>), grid, block, 0, st, a);
         return hipGetLastError();

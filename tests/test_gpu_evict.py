@@ -67,7 +67,7 @@ def _keep_ref(w, n, n_keep, first, recent):
 
 
 @pytest.mark.parametrize("Lk, n_keep, first, recent", [(1, 1, 0, 0), (5, 3, 1, 1), (100, 100, 0, 0), (1000, 999, 4, 64), (1000, 1, 0, 0), (777, 100, 100, 0),
-                                                       (777, 100, 0, 100), (5000, 2500, 4, 128), (40000, 8000, 4, 512), (70001, 35000, 0, 0)])
+                                                       (777, 100, 0, 100), (5000, 2500, 4, 128), (12001, 5000, 4, 64), (20011, 9000, 4, 512), (40000, 8000, 4, 512), (70001, 35000, 0, 0)])
 @pytest.mark.parametrize("kind", ["spread", "ties"])
 def test_what_stays(ic, Lk, n_keep, first, recent, kind):
     say("evict Lk=%d keep=%d first=%d recent=%d %s" % (Lk, n_keep, first, recent, kind))
@@ -96,6 +96,22 @@ def test_what_stays(ic, Lk, n_keep, first, recent, kind):
     # no lengths: every sequence has Lk
     k2, n2, _ = ic.evict_keep(torch.from_numpy(w[:1]).cuda(), n_keep, first, recent)
     assert np.array_equal(k2.cpu().numpy()[0], keep[0]) and int(n2[0]) == n[0]
+
+
+def test_many_long_sequences(ic):
+    """90 of 17001 positions: more parts than compute units, so a workgroup each."""
+    say("evict 90 sequences of 17001")
+    rng = np.random.default_rng(11)
+    B, L, nk = 90, 17001, 6000
+    w = rng.integers(0, 40, (B, L)).astype(np.float32)
+    lens = rng.integers(1, L + 1, B).astype(np.int32)
+    lens[:2] = L, nk + 1
+    keep, n, kept = ic.evict_keep(torch.from_numpy(w).cuda(), nk, 8, 100, seq_lens=torch.from_numpy(lens).cuda())
+    keep, n, kept = keep.cpu().numpy(), n.cpu().numpy(), kept.cpu().numpy()
+    for b in range(B):
+        want = np.array(_keep_ref(w[b], int(lens[b]), nk, 8, 100))
+        assert n[b] == len(want) and np.array_equal(keep[b, :n[b]], want), b
+        assert (keep[b, n[b]:] == -1).all() and np.array_equal(kept[b, :n[b]], w[b][want])
 
 
 def test_a_long_sequence_alone(ic):
