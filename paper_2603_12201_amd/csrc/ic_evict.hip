@@ -85,24 +85,24 @@ __global__ __launch_bounds__(kWeightThreads) void weight_kernel(WeightArgs a)
     }
 }
 
-// The chunks' sums: 32 positions a workgroup, 32 threads to each, whose sums are added in their order.
-__global__ __launch_bounds__(1024) void weight_sum_kernel(WeightArgs a)
+// The chunks' sums: 2^per_log2 threads to a position, whose sums are added in their order.
+__global__ __launch_bounds__(1024) void weight_sum_kernel(WeightArgs a, int per_log2)
 {
-    __shared__ double sums[32][33];
-    const int tid = threadIdx.x, x = tid & 31, y = tid >> 5;
-    const int64_t w0 = (int64_t)blockIdx.x * 32, all = (int64_t)a.B * a.Lk, w = w0 + x;
+    __shared__ double sums[1024];
+    const int tid = threadIdx.x, n_log2 = 10 - per_log2, x = tid & ((1 << n_log2) - 1), y = tid >> n_log2;
+    const int64_t all = (int64_t)a.B * a.Lk, w = ((int64_t)blockIdx.x << n_log2) + x;
     if (w < all) {
         const int64_t b = w / a.Lk;
         const unsigned long long *const part = a.part + (b * a.n_chunks * a.Lk + (w - b * a.Lk));
         double t = 0.0;
 #pragma unroll 4
-        for (int c = y; c < a.n_chunks; c += 32) t += (double)part[(int64_t)c * a.Lk] * 0x1p-48;
-        sums[y][x] = t;
+        for (int c = y; c < a.n_chunks; c += 1 << per_log2) t += (double)part[(int64_t)c * a.Lk] * 0x1p-48;
+        sums[tid] = t;
     }
     __syncthreads();
     if (y == 0 && w < all) {
         double t = a.in ? (double)a.in[w] : 0.0;
-        for (int c = 0; c < 32; ++c) t += sums[c][x];
+        for (int c = 0; c < 1 << per_log2; ++c) t += sums[(c << n_log2) + x];
         a.out[w] = (float)t;
     }
 }
@@ -429,12 +429,12 @@ __global__ __launch_bounds__(256) void compact_kernel(CompactArgs a)
 } // namespace
 
 // Ranges and chunks of a call.  One chunk: the launch writes the weights itself.
-// A range is what LDS holds, as every range's workgroup goes through all of the entries; with no more than two of them per
-// position of a short range the positions cost more, and four times the workgroups take them (32 sequences of 65536 positions,
-// 2048 entries each: 7.8 us against 11.5).
+// A range is what LDS holds, as every range's workgroup goes through all of the entries; with no more than 16 of them per
+// position of a short range that costs less than the positions, and four times the workgroups take them (32 sequences of 65536
+// positions, 2048 entries each: 7.8 us against 11.5; one of 200 000, 32768 entries: 8.7 against 12.6).
 void weight_plan(WeightArgs &a)
 {
-    const int most = (int64_t)a.Tq * a.k_sel <= 2 * kFewRange ? kFewRange : kMaxRange;
+    const int most = (int64_t)a.Tq * a.k_sel <= 16 * kFewRange ? kFewRange : kMaxRange;
     a.range = a.Lk < most ? a.Lk : most;
     a.n_ranges = (a.Lk + a.range - 1) / a.range;
     int chunks = 1;
@@ -458,7 +458,10 @@ hipError_t launch_weight_add(const WeightArgs &a, hipStream_t st)
     if (a.n_chunks > 1) {
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        hipLaunchKernelGGL(weight_sum_kernel, dim3((unsigned)(((int64_t)a.B * a.Lk + 31) / 32)), dim3(1024), 0, st, a);
+        int per_log2 = 1;
+        while (per_log2 < 5 && (1 << per_log2) < a.n_chunks) ++per_log2;
+        const int64_t n = 1024 >> per_log2;
+        hipLaunchKernelGGL(weight_sum_kernel, dim3((unsigned)(((int64_t)a.B * a.Lk + n - 1) / n)), dim3(1024), 0, st, a, per_log2);
     }
     return hipGetLastError();
 }
