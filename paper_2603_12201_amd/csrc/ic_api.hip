@@ -1608,13 +1608,16 @@ struct Kv4Splits {
     int n, len;
     size_t o_bytes, bytes;
 };
-Kv4Splits kv4_splits(const ic_attn_desc *d)
+Kv4Splits kv4_splits(const ic_attn_desc *d, bool merged)
 {
     const int64_t nq = (int64_t)d->B * d->Tq, tiles = (d->k_sel + 31) / 32;
     Kv4Splits r = {1, (int)tiles * 32, 0, 0};
     if (nq < 256) {
-        int64_t ns = 256 / nq, most = (tiles + 3) / 4;
-        if (ns > most) ns = most;
+        const int64_t steps = (tiles + 3) / 4;
+        int64_t ns = 256 / nq;
+        if (ns > steps) ns = steps;
+        // (a merge takes 4 us, a step 2.8: one query of 256 rows 12.3 us in two splits, 10.8 in one; 40 of them 15.3 and 11.3)
+        if (merged && steps - (steps + ns - 1) / ns < 2) ns = 1;
         const int64_t per = (tiles + ns - 1) / ns;
         r.len = (int)per * 32;
         r.n = (int)((tiles + per - 1) / per);
@@ -1678,7 +1681,7 @@ ic_status ic_kv4_read(const ic_kv4_desc *d, const ic_paged_cache *pc, const void
 size_t ic_sparse_attn_kv4_workspace(const ic_attn_desc *d)
 {
     if (check_attn_kv4(d, nullptr, INT32_MAX) != IC_OK && check_attn(d) != IC_OK) return 0;
-    return kv4_splits(d).bytes;
+    return kv4_splits(d, true).bytes;
 }
 
 ic_status ic_sparse_attn_kv4(const ic_attn_desc *d, const ic_paged_cache *pc, int64_t pool_rows, const void *Q, const void *KV4,
@@ -1688,7 +1691,7 @@ ic_status ic_sparse_attn_kv4(const ic_attn_desc *d, const ic_paged_cache *pc, in
     if (s != IC_OK) return s;
     if (!Q || !KV4 || !idx || !O) return fail(IC_ERR_NULL, "Q, KV4, idx and O must not be NULL");
     if (!aligned(Q, 16) || !aligned(KV4, 16) || !aligned(O, 16)) return fail(IC_ERR_SHAPE, "Q, KV4 and O must be 16-byte aligned");
-    const Kv4Splits sp = kv4_splits(d);
+    const Kv4Splits sp = kv4_splits(d, true);
     s = check_ws(workspace, workspace_bytes, sp.bytes);
     if (s != IC_OK) return s;
     ic::Kv4AttnArgs a = kv4_attn_args(d, pc, pool_rows, Q, KV4, idx);
@@ -1739,7 +1742,7 @@ ic_status ic_attn_probs_kv4(const ic_attn_desc *d, const ic_paged_cache *pc, int
     ic::Kv4AttnArgs a = kv4_attn_args(d, pc, pool_rows, Q, KV4, idx);
     a.lse = const_cast<float *>(lse);
     a.probs = probs;
-    const Kv4Splits sp = kv4_splits(d);
+    const Kv4Splits sp = kv4_splits(d, false);
     a.n_splits = sp.n;
     a.split_len = sp.len;
     // (2048 rows each, 768 queries of a sequence each: 140 us with four waves to a query, 156 with one; of one sequence 69 and 77;
