@@ -12,8 +12,9 @@
 // for N(0,1) features the relative error is 0.125, and 0.115 with blocks of 32.
 //
 //   kv4_write_kernel  one wave per row: 16 lanes a block, its maximum by data-parallel moves, codes by the converting
-//                     instruction (ties to the even code).  Bound by memory: 1152 bytes in, 400 out.
-//   kv4_read_kernel   the way back to bf16, exact.
+//                     instruction (ties to the even code).  Bound by memory: 1152 bytes in, 400 out; 131072 rows 41 us,
+//                     4.9 TB/s, what a large copy reaches.
+//   kv4_read_kernel   the way back to bf16, exact: the same rows in 31 us behind the former.
 //   kv4_attn_kernel, kv4_attn_few_kernel
 //                     O = softmax(sm_scale Q K^T) V over the rows that idx names.  See there.
 //   kv4_probs_kernel  the heads' mean of that softmax per selected row, from the log-sum-exps.
@@ -109,7 +110,7 @@ __global__ __launch_bounds__(256) void kv4_write_kernel(Kv4RowsArgs a)
     }
 }
 
-// 2^(byte - 127); 255 makes an infinity of it, times which every code reads as NaN or infinity
+// 2^(byte - 127); 255 makes an infinity of it, with which the conversion gives a NaN for every code
 __device__ __forceinline__ float scale_of(unsigned int byte) { return __uint_as_float(byte << 23); }
 
 // eight codes -> eight bf16
@@ -155,11 +156,13 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4RowsArgs a)
 //       accumulator's 16 registers are the contraction index), so it never leaves the registers.  The A operand wants 8 rows
 //       of one feature per lane: the 4-bit transposing LDS read hands a lane one feature of 16 rows.  Their scales differ by
 //       row, and a conversion has one: V is converted without its scales, and P 2^(e_j), the rows' scales of block j, is what
-//       V's block j is multiplied with.  P is bf16 there (as V is exact, the one rounding of the product: relative 2^-9); a
+//       V's block j is multiplied with.  P is bf16 there (as V is exact, the one rounding of the product: relative 2^-8); a
 //       power of two is then a subtraction from its exponent, two rows an instruction.  It saturates at zero, and P is held
 //       times 2^100 (kMaxE) so that the difference is never negative.
 // The rows' bytes go from memory into LDS without passing through registers; the codes of four tiles, 8 KB each, and the
 // rotary part of one are what a wave has there: bf16 tiles would be three times as large.  No wave waits for another.
+// 32768 queries of 2048 rows: 4.8 ms, 950 TFLOP/s where a plain product of 8192^3 reaches 1141.  Bound by issue: an instruction
+// takes a wave 4.3 to 4.7 clocks, a product 13, and a tile has some 850, 68 of them products (without the fetches 4.2 ms; the fetches alone 2.4).
 // Registers: 256 of O^T, 144 of Q and about 100 more: one wave per SIMD, which issues in order, so the 68 matrix instructions
 // of a tile (32 clocks each) have the rest, about 6 vector instructions each, dealt out between them by hand: a step multiplies
 // K of one tile and V of the tile before it, and works out the softmax of the former during the latter.
@@ -223,10 +226,11 @@ __device__ __forceinline__ void to_lds4(const void *base, unsigned int off, unsi
 }
 
 // What a wave fetches, tile after tile of all of its queries, ahead of what it computes.  In the step of tile n, in this order:
-// the codes of tile n + 2 (8 instructions), the page numbers of n + 4, the entries of idx of n + 6, a wait for all but these 10
-// and the one before them, and when tile n's rotary part has been read that of n + 1 (4) and the exponents of n + 3.  Nothing of
+// the codes of tile n + 2 (8 instructions), the page numbers of n + 4, the entries of idx of n + 6, a wait for all but these
+// and the one before them (kAhead), and when tile n's rotary part has been read that of n + 1 (4) and the exponents of n + 3.  Nothing of
 // it passes through registers, loads return in order, and nothing else loads within the loop over a query's tiles: behind the
-// wait, everything that earlier steps have asked for but their last has arrived.  (Without a page table nothing asks for page numbers.)
+// wait, everything that earlier steps have asked for but their last has arrived.  (Without a page table nothing asks for page numbers.
+// kv4_attn_few_kernel has an order of its own, given there.)
 struct Cursor {
     int q;                                    // query row; n_queries and more: none
     int tile, b, len;                         // len: 0 where there is no such query
@@ -433,7 +437,7 @@ __device__ __forceinline__ f32x4 read4(const f32x16 &o, int i4, float f)
 
 // A product into an accumulator that lives in ordinary registers: O^T takes all of the accumulation registers, and left to
 // itself the compiler puts every accumulator there.  It knows nothing of these instructions' timing: between the conversions that
-// write an operand and the product that reads it there is another product (two wait states are needed), and behind the last
+// write an operand and the product that reads it there is another product or an s_nop (two wait states are needed), and behind the last
 // product comes mfma_settle() (11 wait states before the sum may be read).
 __device__ __forceinline__ void mfma_new(f32x16 &s, bf16x8 x, bf16x8 y) { asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(x), "v"(y)); }
 __device__ __forceinline__ void mfma_add(f32x16 &s, bf16x8 x, bf16x8 y) { asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(x), "v"(y)); }
@@ -727,7 +731,10 @@ __global__ __launch_bounds__(256, 1) void kv4_attn_kernel(Kv4AttnArgs a)
 // to itself each wave had all 512 features, and their sum through LDS took 10 000 clocks).  What bounds a launch is latency:
 // entries, page numbers and rows from memory one after the other, Q meanwhile (36 KB, once in LDS for all four waves: read
 // by each from memory it took 9 000 clocks), then 2.8 us a step of 128 rows.  Measured back to back in a graph: 32 rows of one
-// query 8.4 us (15.3 before these two), 2048 rows in 16 splits 13.4 with their merge, 40 queries of 2048 rows 24.9.
+// query 8.3 us (15.3 before these two), 2048 rows in 16 splits 13.2 with their merge, 40 queries of 2048 rows 24.4.
+// In a step: S, barrier, asks for the rotary part of n + 1, codes of n + 2, page numbers of n + 4 and entries of n + 6, softmax, a wait for
+// all but these, row numbers of n + 3, exponents asked for, barrier, the product with V.  The next step's rotary part then has
+// kAhead instructions behind it.
 struct FewTiles {
     static constexpr int kSlotB = 4 * kCodeB;
     unsigned char code[3][4][kCodeB];         // [ring][wave]

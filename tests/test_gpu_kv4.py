@@ -319,6 +319,25 @@ def test_numbers_that_are_none_stay_with_their_rows(ic):
         assert torch.isfinite(O[:, 1].float()).all() and torch.isfinite(lse[:, 1]).all()
 
 
+@pytest.mark.parametrize("nq", [1, 700])
+def test_a_block_without_numbers_is_none_whatever_its_codes(ic, nq):
+    """The exponent byte 255 beside any codes, and queries of either sign: an infinity of one sign would leave the softmax."""
+    say(f"exponent byte 255, {nq} queries")
+    idx = torch.arange(64, dtype=torch.int32, device="cuda").expand(1, nq, 64).contiguous()
+    for code, block, sign in [(0x00, 0, 1.0), (0x11, 1, -1.0), (0x11, 2, 1.0), (0x99, 3, 1.0), (0x77, 0, -1.0), (0xFF, 2, 1.0)]:
+        kv4 = torch.zeros((1, 64, 400), dtype=torch.uint8, device="cuda")
+        kv4[..., :256] = 0x11
+        kv4[..., 384:388] = 127
+        kv4[0, 5, 64 * block:64 * block + 64] = code
+        kv4[0, 5, 384 + block] = 255
+        Q = torch.full((1, nq, 32, 576), sign, dtype=torch.bfloat16, device="cuda")
+        O, lse = ic.sparse_attn_kv4(Q, kv4, idx, SCALE, want_lse=True)
+        probs = ic.attn_probs_kv4(Q, kv4, idx, SCALE, lse)
+        assert O.isnan().all() and lse.isnan().all() and probs.isnan().all(), (hex(code), block, sign)
+        back = ic.kv4_read(kv4, 1, 64)
+        assert back[0, 5, 128 * block:128 * block + 128].isnan().all() and int(back.isnan().sum()) == 128
+
+
 def test_wide_scales(ic):
     """Blocks whose widths are 2^-60 and 2^60: the scales go into P's exponent."""
     say("wide scales")
