@@ -1,4 +1,5 @@
 """ctypes binding of include/indexcache.h.  Same names as the C entry points, marshalling only."""
+import contextlib
 import ctypes as C
 import os
 
@@ -564,11 +565,19 @@ def distill_loss(probs, sel_scores, want_grad=False, workspace=None, stream=None
 KV4_ROW_BYTES = 400
 
 
+_HERE_AND_NOW = contextlib.nullcontext()
+
+
 def _on(stream):
     """The context in which what a call allocates belongs to its stream (None: the current one)."""
-    import contextlib
+    if stream is None:
+        return _HERE_AND_NOW
     import torch
-    return torch.cuda.stream(stream) if isinstance(stream, torch.cuda.Stream) else contextlib.nullcontext()
+    return torch.cuda.stream(stream) if isinstance(stream, torch.cuda.Stream) else _HERE_AND_NOW
+
+
+def _bytes_of(t):
+    return 0 if t is None else t.numel() * t.element_size()
 
 
 def _current_device():
@@ -659,7 +668,8 @@ def sparse_attn_kv4(Q, kv4, idx, sm_scale, Lk=None, pc=None, want_lse=False, wor
     d, n = _kv4_attn_desc(Q, kv4, idx, sm_scale, Lk, pc)
     with _on(stream):
         if workspace is None:
-            workspace = _workspace(lib().ic_sparse_attn_kv4_workspace(C.byref(d)), Q)
+            need = lib().ic_sparse_attn_kv4_workspace(C.byref(d))
+            workspace = _workspace(need, Q) if need else None
         O = out if out is not None else Q.new_empty((d.B, d.Tq, d.H_q, 512))
         lse = Q.new_empty((d.B, d.Tq, d.H_q), dtype=torch.float32) if want_lse else None
     if out is not None:
@@ -668,7 +678,7 @@ def sparse_attn_kv4(Q, kv4, idx, sm_scale, Lk=None, pc=None, want_lse=False, wor
             raise IcError(Status.ERR_SHAPE, "out %s must be %s" % (tuple(O.shape), (d.B, d.Tq, d.H_q, 512)))
     _same_device(kv4, Q, idx, O, workspace)
     _check(lib().ic_sparse_attn_kv4(C.byref(d), _ref(pc), n, _ptr(Q), _ptr(kv4), _ptr(idx), _ptr(O), _ptr(lse), _ptr(workspace),
-                                    workspace.numel() * workspace.element_size(), _stream(stream)))
+                                    _bytes_of(workspace), _stream(stream)))
     return (O, lse) if want_lse else O
 
 
@@ -702,10 +712,12 @@ def attn_weight_add(probs, idx, weight, out=None, workspace=None, stream=None):
     _same_device(weight, probs, idx, out, workspace)
     Lk = weight.shape[1]
     if workspace is None:
-        with _on(stream):
-            workspace = _workspace(lib().ic_attn_weight_add_workspace(B, Tq, k, Lk), weight)
+        need = lib().ic_attn_weight_add_workspace(B, Tq, k, Lk)
+        if need:
+            with _on(stream):
+                workspace = _workspace(need, weight)
     _check(lib().ic_attn_weight_add(B, Tq, k, Lk, _ptr(probs), _ptr(idx), _ptr(weight), _ptr(out), _ptr(workspace),
-                                    workspace.numel() * workspace.element_size(), _stream(stream)))
+                                    _bytes_of(workspace), _stream(stream)))
     return out
 
 
@@ -724,12 +736,13 @@ def evict_keep(weight, n_keep, n_first=0, n_recent=0, seq_lens=None, workspace=N
         raise IcError(Status.ERR_SHAPE, "n_keep=%d must be positive" % n_keep)
     with _on(stream):
         if workspace is None:
-            workspace = _workspace(lib().ic_evict_keep_workspace(B, Lk), weight)
+            need = lib().ic_evict_keep_workspace(B, Lk)
+            workspace = _workspace(need, weight) if need else None
         keep = weight.new_empty((B, n_keep), dtype=torch.int32)
         lens = weight.new_empty((B,), dtype=torch.int32)
         kept = weight.new_empty((B, n_keep))
     _check(lib().ic_evict_keep(B, Lk, _ptr(weight), _ptr(seq_lens), n_keep, n_first, n_recent, _ptr(keep), _ptr(lens), _ptr(kept),
-                               _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
+                               _ptr(workspace), _bytes_of(workspace), _stream(stream)))
     return keep, lens, kept
 
 
