@@ -393,18 +393,26 @@ __global__ __launch_bounds__(kEvictThreads) void evict_part_kernel(EvictArgs a)
 
 constexpr int kMoveRows = 32;                 // rows of a workgroup
 
-template <typename T>
+// PAST: past the caches (launch_compact())
+template <typename T, bool PAST>
 __device__ __forceinline__ void move_rows(const CompactArgs &a, int c, const int64_t *src, const int64_t *dst, int tid)
 {
     const int per = a.row_bytes[c] / (int)sizeof(T), total = kMoveRows * per;
     for (int i = tid; i < total; i += 256) {
         const int r = i / per, k = i - r * per;
         const int64_t s = src[r], d = dst[r];
-        if (s >= 0 && s < a.src_rows[c] && d >= 0 && d < a.dst_rows[c])
-            *(T *)(a.dst[c] + d * a.row_bytes[c] + (int64_t)k * sizeof(T)) = *(const T *)(a.src[c] + s * a.row_bytes[c] + (int64_t)k * sizeof(T));
+        if (s >= 0 && s < a.src_rows[c] && d >= 0 && d < a.dst_rows[c]) {
+            const T x = *((const T *)(a.src[c] + s * a.row_bytes[c]) + k);
+            T *const to = (T *)(a.dst[c] + d * a.row_bytes[c]) + k;
+            if (PAST)
+                __builtin_nontemporal_store(x, to);
+            else
+                *to = x;
+        }
     }
 }
 
+template <bool PAST>
 __global__ __launch_bounds__(256) void compact_kernel(CompactArgs a)
 {
     __shared__ int64_t src[kMoveRows], dst[kMoveRows];
@@ -421,9 +429,9 @@ __global__ __launch_bounds__(256) void compact_kernel(CompactArgs a)
     __syncthreads();
     const uintptr_t any = (uintptr_t)a.src[c] | (uintptr_t)a.dst[c] | (uintptr_t)a.row_bytes[c];
     if (any % 16 == 0)
-        move_rows<u32x4>(a, c, src, dst, tid);
+        move_rows<u32x4, PAST>(a, c, src, dst, tid);
     else
-        move_rows<unsigned int>(a, c, src, dst, tid);
+        move_rows<unsigned int, PAST>(a, c, src, dst, tid);
 }
 
 } // namespace
@@ -503,7 +511,15 @@ hipError_t launch_evict_keep(EvictArgs a, hipStream_t st)
 hipError_t launch_compact(const CompactArgs &a, hipStream_t st)
 {
     const int per_seq = (a.n_keep + kMoveRows - 1) / kMoveRows;
-    hipLaunchKernelGGL(compact_kernel, dim3((unsigned)(a.B * per_seq), (unsigned)a.n_caches), dim3(256), 0, st, a);
+    const dim3 grid((unsigned)(a.B * per_seq), (unsigned)a.n_caches), block(256);
+    int64_t bytes = 0;
+    for (int c = 0; c < a.n_caches; ++c) bytes += (int64_t)a.B * a.n_keep * a.row_bytes[c];
+    // What is more than the last cache holds (256 MB) goes past the caches: the step behind would not find it there, and it is faster
+    // (344 MB 144 us against 150).
+    if (bytes > (int64_t)256 << 20)
+        hipLaunchKernelGGL((compact_kernel<true>), grid, block, 0, st, a);
+    else
+        hipLaunchKernelGGL((compact_kernel<false>), grid, block, 0, st, a);
     return hipGetLastError();
 }
 

@@ -159,6 +159,21 @@ def test_rows_move_to_their_places(ic, sp, dp):
         assert np.array_equal(c.cpu().numpy(), want)
 
 
+def test_more_rows_than_the_caches_hold(ic):
+    """Over 256 MB to write, in rows of 1152 and of 20 bytes."""
+    say("compact 2 x 119001 rows of 1152 and 20 bytes")
+    g = torch.Generator(device="cuda").manual_seed(3)
+    B, Lk, n_keep = 2, 130000, 119001
+    keep = torch.stack([torch.randperm(Lk, generator=g, device="cuda")[:n_keep].sort()[0] for _ in range(B)])
+    keep[1, -3:] = -1
+    src = [torch.randint(-(1 << 31), 1 << 31, (B, Lk, w // 4), generator=g, device="cuda").int() for w in (1152, 20)]
+    dst = [torch.full((B, n_keep, w // 4), 77, dtype=torch.int32, device="cuda") for w in (1152, 20)]
+    ic.cache_compact(list(zip(src, dst)), keep.int(), Lk)
+    for a, c in zip(src, dst):
+        assert torch.equal(c[0], a[0][keep[0]]) and torch.equal(c[1, :-3], a[1][keep[1, :-3]])
+        assert bool((c[1, -3:] == 77).all())
+
+
 def test_compaction_keeps_to_its_buffers(ic):
     """A page table that names pages the pools do not have."""
     table = torch.tensor([[1, 5, -3]], dtype=torch.int32, device="cuda")
