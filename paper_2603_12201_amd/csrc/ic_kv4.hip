@@ -392,6 +392,21 @@ struct Fetch {
         }
         asm volatile("s_waitcnt vmcnt(10)" ::: "memory");                   // (tile 0 has arrived)
     }
+    // the same where there is one step, which then asks for nothing
+    __device__ __forceinline__ void begin_one(int lane, unsigned int (&ok)[3])
+    {
+        ask_ids(0, lane);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if (PAGED) {
+            ask_pages(0, entry(0, lane));
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        }
+        ok[0] = find_rows(0, entry(0, lane), page(0, lane), lane);
+        ok[1] = ok[2] = 0;
+        ask_codes(code_slot(0), lane);
+        ask_ropes(0, lane);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
 };
 
 // Over the lanes l and l + 32.
@@ -731,7 +746,8 @@ __global__ __launch_bounds__(256, 1) void kv4_attn_kernel(Kv4AttnArgs a)
 // to itself each wave had all 512 features, and their sum through LDS took 10 000 clocks).  What bounds a launch is latency:
 // entries, page numbers and rows from memory one after the other, Q meanwhile (36 KB, once in LDS for all four waves: read
 // by each from memory it took 9 000 clocks), then 2.8 us a step of 128 rows.  Measured back to back in a graph: 32 rows of one
-// query 8.3 us (15.3 before these two), 2048 rows in 16 splits 13.2 with their merge, 40 queries of 2048 rows 24.4.
+// query 7.3 us (15.3 before these two), 2048 rows in 16 splits 12.4 with their merge, 40 queries of 2048 rows 24.3.  The last
+// step asks for nothing (a microsecond of it).
 // In a step: S, barrier, asks for the rotary part of n + 1, codes of n + 2, page numbers of n + 4 and entries of n + 6, softmax, a wait for
 // all but these, row numbers of n + 3, exponents asked for, barrier, the product with V.  The next step's rotary part then has
 // kAhead instructions behind it.
@@ -786,7 +802,11 @@ __global__ __launch_bounds__(256, 1) void kv4_attn_few_kernel(Kv4AttnArgs a)
     unsigned char *const q_lds = &lds.code[2][0][0];
     ask_q(a, q, (unsigned)__builtin_amdgcn_readfirstlane((int)lds_offset(q_lds)), wave, lane);
     unsigned int n = 0, slot = 0, ok[3];
-    f.begin(lane, ok);
+    const int n_steps = (f.n_tiles + 3) / 4;
+    if (n_steps > 1)
+        f.begin(lane, ok);
+    else
+        f.begin_one(lane, ok);
     meet();                                    // (Q was asked for before what begin() has waited for)
     bf16x8 ql[8][4], qr[4];
     read_q(q_lds, lane, ql, qr);
@@ -798,7 +818,6 @@ __global__ __launch_bounds__(256, 1) void kv4_attn_few_kernel(Kv4AttnArgs a)
     float m = -INFINITY, l = 0.f;
     const int kr = tile_row(l32), gr = 16 * (g ^ (kr & 15)), rr = 16 * (g ^ (kr >> 1 & 7));
     const int vr = tile_row(8 * ((lane & 15) >> 2) + 4 * g + (lane & 3)), r16 = 16 * (vr & 15);
-    const int n_steps = (f.n_tiles + 3) / 4;
     auto k_at = [&](unsigned int at) __attribute__((always_inline)) { return &lds.code[at][wave][kr * 256]; };
     u32x4 kc[3];                               // K's codes, chunks j in [j % 3]; of the tile that comes 0 and 1, and its exponents
     kc[0] = *(const u32x4 *)(k_at(0) + gr);
@@ -871,10 +890,13 @@ __global__ __launch_bounds__(256, 1) void kv4_attn_few_kernel(Kv4AttnArgs a)
 #pragma unroll
         for (int w = 0; w < 4; ++w) tops[w] = lds.top[n & 1][w][l32];
         const unsigned int two = slot == 0 ? 2 : slot - 1;
-        f.ask_ropes(n + 1, lane);
-        f.ask_codes((unsigned)__builtin_amdgcn_readfirstlane((int)(f.code0 + two * FewTiles::kSlotB)), lane);
-        f.ask_pages(n + 4, f.entry(n + 4, lane));
-        f.ask_ids(n + 6, lane);
+        const bool more = t + 1 < n_steps;
+        if (more) {
+            f.ask_ropes(n + 1, lane);
+            f.ask_codes((unsigned)__builtin_amdgcn_readfirstlane((int)(f.code0 + two * FewTiles::kSlotB)), lane);
+            f.ask_pages(n + 4, f.entry(n + 4, lane));
+            f.ask_ids(n + 6, lane);
+        }
         top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
         if (__ballot(top > m + a.lag) != 0ull) {                             // (the same in every wave)
             const float mn = fmaxf(m, top), keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
@@ -892,11 +914,13 @@ __global__ __launch_bounds__(256, 1) void kv4_attn_few_kernel(Kv4AttnArgs a)
         }
         lds.p[n & 1][wave][0][lane] = p[0];
         lds.p[n & 1][wave][1][lane] = p[1];
-        ok[0] = ok[1];
-        ok[1] = ok[2];
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(f.kAhead + 3) : "memory");  // (this step's: the page numbers of n + 3 were asked for a step ago)
-        ok[2] = f.find_rows(n + 3, f.entry(n + 3, lane), f.page(n + 3, lane), lane);
-        f.advance();
+        if (more) {
+            ok[0] = ok[1];
+            ok[1] = ok[2];
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(f.kAhead + 3) : "memory");  // (this step's: the page numbers of n + 3 were asked for a step ago)
+            ok[2] = f.find_rows(n + 3, f.entry(n + 3, lane), f.page(n + 3, lane), lane);
+            f.advance();
+        }
         meet();
         // O^T += V^T P^T of the four tiles, this wave's features.  (A tile without rows: its P is 0, and any code is a number.)
         typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
