@@ -319,6 +319,60 @@ def test_numbers_that_are_none_stay_with_their_rows(ic):
         assert torch.isfinite(O[:, 1].float()).all() and torch.isfinite(lse[:, 1]).all()
 
 
+@pytest.mark.parametrize("nq", [2, 600])
+def test_a_position_named_more_than_once_counts_as_often(ic, nq):
+    say(f"entries that repeat, {nq} queries")
+    rng = np.random.default_rng(nq)
+    Lk, k = 50, 200
+    x = rows_of(6, Lk, wide=False)
+    packed = kv4_ref.pack(bits(x))
+    Q = torch.randn((1, nq, 32, 576), generator=torch.Generator().manual_seed(6)).to(torch.bfloat16)
+    idx = rng.integers(0, Lk, (1, nq, k)).astype(np.int32)
+    idx[0, 0] = 7
+    kv4, at = torch.from_numpy(packed).cuda().view(1, Lk, 400), torch.from_numpy(idx).cuda()
+    O, lse = ic.sparse_attn_kv4(Q.cuda(), kv4, at, SCALE, want_lse=True)
+    probs = ic.attn_probs_kv4(Q.cuda(), kv4, at, SCALE, lse)
+    weight = ic.attn_weight_add(probs, at, torch.zeros((1, Lk), device="cuda"))
+    rows = kv4_ref.unpack(packed)
+    for t in (0, 1, nq - 1):
+        check_query(O[0, t], lse[0, t], probs[0, t], kv4_ref.bf16_bits_to_f64(bits(Q))[0, t], rows[idx[0, t]], np.ones(k, dtype=bool))
+    want = np.zeros(Lk)
+    np.add.at(want, idx.ravel(), probs.double().cpu().numpy().ravel())
+    # each entry down to 2^-48, the sum rounded to fp32
+    assert np.all(np.abs(weight[0].double().cpu().numpy() - want) <= nq * k * 2.0 ** -48 + want * 2.0 ** -24)
+
+
+def test_calls_at_once_on_two_streams(ic):
+    """The same operators on two streams with nothing between them: what each leaves is what it leaves alone."""
+    say("two streams at once")
+    jobs = []
+    for i, (B, k) in enumerate([(3, 700), (5, 300)]):
+        Lk = 900
+        kv4 = torch.from_numpy(kv4_ref.pack(bits(rows_of(40 + i, B * Lk, wide=False)))).cuda().view(B, Lk, 400)
+        Q = torch.randn((B, 1, 32, 576), generator=torch.Generator().manual_seed(i)).to(torch.bfloat16).cuda()
+        idx = torch.stack([torch.randperm(Lk, generator=torch.Generator().manual_seed(9 * i + b))[:k].sort()[0].int() for b in range(B)])[:, None].contiguous().cuda()
+        jobs.append((Q, kv4, idx))
+
+    def run(Q, kv4, idx):
+        O, lse = ic.sparse_attn_kv4(Q, kv4, idx, SCALE, want_lse=True)
+        p = ic.attn_probs_kv4(Q, kv4, idx, SCALE, lse)
+        w = ic.attn_weight_add(p, idx, torch.zeros((Q.shape[0], kv4.shape[1]), device="cuda"))
+        return [O, lse, p, w] + list(ic.evict_keep(w, 400, 4, 50))
+
+    alone = [run(*j) for j in jobs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in jobs]
+    for _ in range(4):
+        got = []
+        for st, j in zip(streams, jobs):
+            with torch.cuda.stream(st):
+                got.append([run(*j) for _ in range(3)])
+        torch.cuda.synchronize()
+        for want, runs in zip(alone, got):
+            for r in runs:
+                assert all(torch.equal(a, b) for a, b in zip(want, r))
+
+
 @pytest.mark.parametrize("nq", [1, 700])
 def test_a_block_without_numbers_is_none_whatever_its_codes(ic, nq):
     """The exponent byte 255 beside any codes, and queries of either sign: an infinity of one sign would leave the softmax."""
