@@ -2052,7 +2052,8 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(AttnArgs a)
         m = mt;
         l = lt;
     }
-    if (tid == 0 && a.lse) a.lse[qrow * a.H_q + h] = (l > 0.f) ? (m + __builtin_log2f(l)) * 0.6931471805599453f : -INFINITY;
+    // (a sum that is not a number is no empty row)
+    if (tid == 0 && a.lse) a.lse[qrow * a.H_q + h] = l == 0.f ? -INFINITY : (m + __builtin_log2f(l)) * 0.6931471805599453f;
 }
 
 template <int D_V, int SLOTS, bool WIDE>
