@@ -47,9 +47,12 @@ __device__ __forceinline__ int64_t kv4_row(const PagedView &pv, int b, int s, in
     return r >= 0 && r < pool_rows ? r : -1;
 }
 
-__device__ __forceinline__ int seq_len(const PagedView &pv, int b, int Lk)
+// Row of the cache that row i of sequence b goes to, or -1.
+__device__ __forceinline__ int64_t row_of(const Kv4RowsArgs &a, int b, int i)
 {
-    return pv.seq_lens ? min(pv.seq_lens[b], Lk) : Lk;
+    const int n = a.pv.seq_lens ? a.pv.seq_lens[b] : a.Lk, len = min(n, a.Lk);
+    const int64_t pos = a.pv.seq_lens ? (int64_t)n - a.Tn + i : a.pos0 + i;   // (n may be beyond Lk: the rows there are left out)
+    return pos < 0 || pos >= len ? -1 : kv4_row(a.pv, b, (int)pos, len, a.Lk, a.pool_rows);
 }
 
 // (by value: a bit cast of a vector's element takes the vector's first)
@@ -76,9 +79,7 @@ __global__ __launch_bounds__(256) void kv4_write_kernel(Kv4RowsArgs a)
     const int64_t n = (int64_t)a.B * a.Tn, stride = (int64_t)gridDim.x * 4;
     for (int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); r < n; r += stride) {
         const int b = (int)(r / a.Tn), i = (int)(r - (int64_t)b * a.Tn);
-        const int len = seq_len(a.pv, b, a.Lk);
-        const int64_t pos = a.pv.seq_lens ? (int64_t)len - a.Tn + i : a.pos0 + i;
-        const int64_t row = pos < 0 || pos >= len ? -1 : kv4_row(a.pv, b, (int)pos, len, a.Lk, a.pool_rows);
+        const int64_t row = row_of(a, b, i);
         if (row < 0) continue;                                              // (wave-uniform)
         const unsigned short *src = (const unsigned short *)a.rows + r * kRow;
         const u32x4 x = *(const u32x4 *)(src + 8 * lane);                   // features 8 lane ..: 16 lanes a block
@@ -129,9 +130,7 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4RowsArgs a)
     const int64_t n = (int64_t)a.B * a.Tn, stride = (int64_t)gridDim.x * 4;
     for (int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); r < n; r += stride) {
         const int b = (int)(r / a.Tn), i = (int)(r - (int64_t)b * a.Tn);
-        const int len = seq_len(a.pv, b, a.Lk);
-        const int64_t pos = a.pv.seq_lens ? (int64_t)len - a.Tn + i : a.pos0 + i;
-        const int64_t row = pos < 0 || pos >= len ? -1 : kv4_row(a.pv, b, (int)pos, len, a.Lk, a.pool_rows);
+        const int64_t row = row_of(a, b, i);
         unsigned short *dst = (unsigned short *)a.out + r * kRow;
         u32x4 v = u32x4{0u, 0u, 0u, 0u};
         unsigned int rope = 0;

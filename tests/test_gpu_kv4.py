@@ -538,3 +538,29 @@ def test_captured_and_on_another_stream(ic):
         torch.cuda.synchronize()
         for a, b in zip(mine, want):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("page", [0, 64])
+def test_lengths_beyond_the_bound_leave_out_the_rows_behind_it(ic, page):
+    """Row i goes to seq_lens[b] - Tn + i, also where that is behind Lk: such rows are left out, the others keep their positions."""
+    B, Lk, Tn = 4, 100, 6
+    lens = [100, 103, 106, 1 << 30]
+    say("write behind the bound, page %d" % page)
+    x = rows_of(31, B * Tn).reshape(B, Tn, 576)
+    p = kv4_ref.pack(bits(x))
+    pg = Paged(ic, [Lk] * B, Lk, page) if page else None
+    n = pg.n_rows if page else B * Lk
+    pc = ic.paged_cache(torch.tensor(lens, dtype=torch.int32, device="cuda"), pg.dev[1] if page else None, page)
+    kv4 = torch.full((n, 400) if page else (B, Lk, 400), 0xAB, dtype=torch.uint8, device="cuda")
+    want, back = np.full((n, 400), 0xAB, dtype=np.uint8), np.zeros((B, Tn, 576))
+    for b in range(B):
+        for i in range(Tn):
+            s = lens[b] - Tn + i
+            if s < Lk:
+                want[pg.row(b, s) if page else b * Lk + s] = p[b, i]
+                back[b, i] = kv4_ref.unpack(p[b, i])
+    ic.kv4_write(x.cuda(), kv4, Lk=Lk, pc=pc)
+    out = ic.kv4_read(kv4, B, Tn, Lk=Lk, pc=pc)
+    torch.cuda.synchronize()
+    assert np.array_equal(kv4.cpu().numpy().reshape(n, 400), want)
+    assert np.array_equal(out.cpu().double().numpy(), back)
