@@ -36,6 +36,10 @@ constexpr int kTile = 32;
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// Whether the sum l of a row by the reference m has the log-sum-exp of an empty row: nothing counted, or no score above -inf.  (A
+// sum that is not a number beside finite scores has not: a probability worked out from -inf would be infinite for all of them.)
+__device__ __forceinline__ bool empty_sum(float l, float m) { return l == 0.f || m == -INFINITY; }
+
 // layer of query gq of a launch (several layers share one where they have a few thousand queries together: 32 bits do; the
 // division in 64 bits costs every workgroup about 1 us before its first load)
 __device__ __forceinline__ int layer_of(const AttnArgs &a, int64_t gq)
@@ -235,7 +239,7 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a)
             ml[1] = l_tot;
         } else if (a.lse) {
             a.lse[qrow * a.H_q + head] =
-                (l_tot > 0.f) ? (m_run + __builtin_log2f(l_tot)) * 0.6931471805599453f : -INFINITY;
+                empty_sum(l_tot, m_run) ? -INFINITY : (m_run + __builtin_log2f(l_tot)) * 0.6931471805599453f;
         }
     }
     // a split stores its own normalised output; the merge weighs the splits by their share of the total row sum
@@ -720,7 +724,7 @@ __global__ __launch_bounds__(256, 1) void attn_slab_kernel(AttnArgs a)
                 }
             } else {
                 if (wave == 0 && hh == 0 && l32 < a.H_q && a.lse)
-                    a.lse[qrow * a.H_q + l32] = l_head > 0.f ? (float)(((double)m_head + (double)__builtin_log2f(l_head)) * 0.6931471805599453) : -INFINITY;
+                    a.lse[qrow * a.H_q + l32] = empty_sum(l_head, m_head) ? -INFINITY : (float)(((double)m_head + (double)__builtin_log2f(l_head)) * 0.6931471805599453);
             }
             // accumulator element i belongs to head 8 (i / 4) + 4 hh + i % 4: the sums of the lane's
             // 16 heads come straight from the four waves' partials (independent 16-byte reads; a
@@ -1244,7 +1248,7 @@ __device__ __forceinline__ void dense_rows(const AttnArgs &a, const DenseArgs &d
                 // (in 64 bits: the reference of 32 keys leaves a larger logarithm, and so a coarser sum, than that of the row form's 64)
                 if (a.lse && w == 0 && half == 0 && k.R0 + 32 * r + c32 < k.n_rows)
                     a.lse[row0 + 32 * r + c32] =
-                        l > 0.f ? (float)(((double)fac[2 * kDenseRows + 32 * r + c32] + (double)__builtin_log2f(l)) * 0.6931471805599453) : -INFINITY;
+                        empty_sum(l, fac[2 * kDenseRows + 32 * r + c32]) ? -INFINITY : (float)(((double)fac[2 * kDenseRows + 32 * r + c32] + (double)__builtin_log2f(l)) * 0.6931471805599453);
                 unroll<16>([&](auto q_c) __attribute__((always_inline)) {
                     constexpr int nb = decltype(q_c)::value >> 2, qd = decltype(q_c)::value & 3;
                     s16x4 o;
@@ -1811,7 +1815,7 @@ __global__ __launch_bounds__(512, 2) void attn_stream_kernel(AttnArgs a, RestArg
         const int64_t row = tensor_row(gq, layer, b);
         if (w == 0 && half == 0 && row_l < a.H_q && a.lse) {
             // (in 64 bits: the reference of 16 keys leaves a larger logarithm, and so a coarser sum, than that of more)
-            a.lse[row * a.H_q + row_l] = l > 0.f ? (float)(((double)m_c + (double)__builtin_log2f(l)) * 0.6931471805599453) : -INFINITY;
+            a.lse[row * a.H_q + row_l] = empty_sum(l, m_c) ? -INFINITY : (float)(((double)m_c + (double)__builtin_log2f(l)) * 0.6931471805599453);
         }
         constexpr int OSTR = 256 + 16;
         static_assert(32 * OSTR <= 8 * ROWB, "32 heads of 256 bytes");
