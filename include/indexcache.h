@@ -295,7 +295,8 @@ ic_status ic_attn_probs_kv4(const ic_attn_desc *desc, const ic_paged_cache *pc, 
  * ic_attn_weight_add: what each position received,
  *     weight[b,s] = weight_in[b,s] + sum over t, m with idx[b,t,m] = s of probs[b,t,m]
  *   probs, idx [B,Tq,k_sel] as ic_attn_probs and ic_indexer_topk leave them (entries outside [0, Lk) are skipped, equal
- *   entries of a row all count); weight_in [B,Lk] fp32, nullable (zeros), may be weight itself; weight [B,Lk] fp32 out.
+ *   entries of a row all count); weight_in [B,Lk] fp32, nullable (zeros), may be weight itself; weight [B,Lk] fp32 out,
+ *   which must not overlap anything else that is read.
  *   A probability below 0 or not a number counts as 0, one above 1 as 1; each is taken to 2^-48, and their sum is the same
  *   whatever the order (a row's probabilities at one position must add up to less than 2).  workspace: ic_attn_weight_add_workspace() bytes (0 for a few rows).
  *
@@ -305,6 +306,7 @@ ic_status ic_attn_probs_kv4(const ic_attn_desc *desc, const ic_paged_cache *pc, 
  *   largest).  n_first + n_recent <= n_keep <= Lk.
  *   keep [B,n_keep] int32 out: the positions in ASCENDING order, then -1;  keep_lens [B] int32 out: their number, the new
  *   seq_lens;  keep_weight [B,n_keep] fp32 out, nullable: weight at those positions (0 behind them), the new weight.
+ *   None of the three may overlap another, weight or seq_lens (IC_ERR_SHAPE): the new lengths and weights are buffers of their own.
  *   workspace: ic_evict_keep_workspace(B, Lk) bytes.
  *
  * ic_cache_compact: rows of n_caches caches (host array, at most IC_MAX_MOVE_CACHES; each with rows of its own width, a

@@ -1790,6 +1790,11 @@ ic_status ic_attn_weight_add(int32_t B, int32_t Tq, int32_t k_sel, int32_t Lk, c
     if (!probs || !idx || !weight) return fail(IC_ERR_NULL, "probs, idx and weight must not be NULL");
     s = check_ws(workspace, workspace_bytes, ws);
     if (s != IC_OK) return s;
+    const size_t entries = (size_t)B * Tq * k_sel * 4, positions = (size_t)B * Lk * 4;
+    const Range out = {(const char *)weight, positions};
+    if (out.meets({(const char *)probs, entries}) || out.meets({(const char *)idx, entries}) ||
+        (weight_in && weight_in != weight && out.meets({(const char *)weight_in, positions})))
+        return fail(IC_ERR_SHAPE, "weight overlaps what is read (it may be weight_in, the whole of it)");
     a.probs = probs;
     a.idx = idx;
     a.in = weight_in;
@@ -1818,6 +1823,14 @@ ic_status ic_evict_keep(int32_t B, int32_t Lk, const float *weight, const int32_
     if (!weight || !keep || !keep_lens) return fail(IC_ERR_NULL, "weight, keep and keep_lens must not be NULL");
     ic_status s = check_ws(workspace, workspace_bytes, ic_evict_keep_workspace(B, Lk));
     if (s != IC_OK) return s;
+    // (workgroups read lengths and weights while others write)
+    const size_t kept = (size_t)B * n_keep * 4;
+    const Range buf[] = {{(const char *)keep, kept}, {(const char *)keep_lens, (size_t)B * 4}, {(const char *)keep_weight, keep_weight ? kept : 0},
+                         {(const char *)weight, (size_t)B * Lk * 4}, {(const char *)seq_lens, seq_lens ? (size_t)B * 4 : 0}};
+    for (int i = 0; i < 3; ++i)
+        for (int j = i + 1; j < 5; ++j)
+            if (buf[i].n != 0 && buf[j].n != 0 && buf[i].meets(buf[j]))
+                return fail(IC_ERR_SHAPE, "keep, keep_lens and keep_weight must not overlap weight, seq_lens or each other");
     ic::EvictArgs a;
     memset(&a, 0, sizeof a);
     a.weight = weight;

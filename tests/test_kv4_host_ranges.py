@@ -1,0 +1,44 @@
+"""What the eviction entry points refuse about where their buffers lie and how long their sequences are, before anything is launched;
+no GPU needed (addresses that nothing reads)."""
+import ctypes as C
+
+import pytest
+
+FAR = 1 << 30
+
+
+@pytest.fixture(scope="module")
+def ic():
+    import paper_2603_12201_amd as m
+    m.lib()
+    return m
+
+
+def _evict(ic, B=2, Lk=1000, n_keep=400, weight=FAR, lens=2 * FAR, keep=3 * FAR, keep_lens=4 * FAR, kept=5 * FAR):
+    return ic.lib().ic_evict_keep(B, Lk, weight, lens, n_keep, 4, 16, keep, keep_lens, kept, 6 * FAR, 1 << 40, None)
+
+
+def test_what_stays_is_not_written_over_what_is_read(ic):
+    """Workgroups read lengths and weights while others write."""
+    S = ic.Status
+    for lens in (2 * FAR, None):                                                 # one sequence of a length in place, lengths in place
+        assert _evict(ic, lens=lens, kept=FAR) == S.ERR_SHAPE                    # the weights in place
+        assert _evict(ic, lens=lens, kept=FAR + 4 * (2 * 1000 - 1)) == S.ERR_SHAPE   # their last element
+        assert _evict(ic, lens=lens, keep=FAR) == S.ERR_SHAPE
+        assert _evict(ic, lens=lens, keep_lens=FAR + 4 * 1000) == S.ERR_SHAPE
+        assert _evict(ic, lens=lens, keep=3 * FAR, kept=3 * FAR + 4 * (2 * 400 - 1)) == S.ERR_SHAPE
+        assert _evict(ic, lens=lens, keep_lens=3 * FAR + 8) == S.ERR_SHAPE
+        assert _evict(ic, lens=lens, keep_lens=5 * FAR) == S.ERR_SHAPE
+    assert _evict(ic, keep_lens=2 * FAR) == S.ERR_SHAPE                          # the lengths in place
+    assert _evict(ic, keep_lens=2 * FAR + 4) == S.ERR_SHAPE
+    assert _evict(ic, keep=2 * FAR - 8 * 400 + 4) == S.ERR_SHAPE and _evict(ic, kept=2 * FAR) == S.ERR_SHAPE
+    assert b"overlap" in ic.lib().ic_last_error()
+
+
+def test_weights_are_not_written_over_what_is_read(ic):
+    def add(probs=FAR, idx=2 * FAR, w_in=3 * FAR, w=4 * FAR):
+        return ic.lib().ic_attn_weight_add(2, 3, 64, 1000, probs, idx, w_in, w, 6 * FAR, 1 << 40, None)
+
+    S = ic.Status
+    assert add(w=FAR) == S.ERR_SHAPE and add(w=FAR + 4 * (2 * 3 * 64 - 1)) == S.ERR_SHAPE and add(w=2 * FAR - 4 * (2 * 1000 - 1)) == S.ERR_SHAPE
+    assert add(w=3 * FAR + 4) == S.ERR_SHAPE and add(w=3 * FAR - 4 * 1000) == S.ERR_SHAPE   # (the same address is in place, and allowed)
