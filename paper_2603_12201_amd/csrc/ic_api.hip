@@ -1592,7 +1592,8 @@ ic_status kv4_rows(const ic_kv4_desc *d, const ic_paged_cache *pc, ic::Kv4RowsAr
     return IC_OK;
 }
 
-ic_status check_attn_kv4(const ic_attn_desc *d, const ic_paged_cache *pc, int64_t pool_rows)
+// (what does not depend on a cache)
+ic_status check_kv4_layout(const ic_attn_desc *d)
 {
     ic_status s = check_attn(d);
     if (s != IC_OK) return s;
@@ -1600,7 +1601,13 @@ ic_status check_attn_kv4(const ic_attn_desc *d, const ic_paged_cache *pc, int64_
         return fail(IC_ERR_UNSUPPORTED, "a 4-bit cache holds rows of 576 with values 0..511 (d_qk=%d d_v=%d v_off=%d row_elems=%d)", d->d_qk, d->d_v,
                     d->v_off, d->row_elems);
     if (d->k_sel > 1 << 24) return fail(IC_ERR_UNSUPPORTED, "k_sel=%d exceeds %d", d->k_sel, 1 << 24);
-    return check_kv4_cache(pc, d->B, d->Lk, pool_rows);
+    return IC_OK;
+}
+
+ic_status check_attn_kv4(const ic_attn_desc *d, const ic_paged_cache *pc, int64_t pool_rows)
+{
+    ic_status s = check_kv4_layout(d);
+    return s != IC_OK ? s : check_kv4_cache(pc, d->B, d->Lk, pool_rows);
 }
 
 // Splits of a query, so that few of them still use all 256 compute units; a split has a tile for each of a workgroup's waves.
@@ -1680,7 +1687,7 @@ ic_status ic_kv4_read(const ic_kv4_desc *d, const ic_paged_cache *pc, const void
 
 size_t ic_sparse_attn_kv4_workspace(const ic_attn_desc *d)
 {
-    if (check_attn_kv4(d, nullptr, INT32_MAX) != IC_OK && check_attn(d) != IC_OK) return 0;
+    if (check_kv4_layout(d) != IC_OK) return 0;
     return kv4_splits(d, true).bytes;
 }
 

@@ -168,3 +168,14 @@ def test_the_reference_row_by_hand():
     f[5] = np.inf
     bits[0] = (f.view(np.uint32) >> 16).astype(np.uint16)
     assert kv4_ref.pack(bits)[0, 384] == 255 and np.isnan(kv4_ref.unpack(kv4_ref.pack(bits))[0, :128]).all()
+
+
+def test_a_layout_that_the_call_refuses_needs_no_workspace(ic):
+    """With 2048 rows, which are split and need one otherwise."""
+    L, S = ic.lib(), ic.Status
+    assert L.ic_sparse_attn_kv4_workspace(C.byref(_ad(ic, k_sel=2048))) > 0
+    for bad in (dict(k_sel=2048, d_qk=64, d_v=64, v_off=64, row_elems=128), dict(k_sel=2048, row_elems=640), dict(k_sel=(1 << 24) + 1),
+                dict(k_sel=2048, sm_scale=-1.0)):
+        d = _ad(ic, **bad)
+        assert L.ic_sparse_attn_kv4_workspace(C.byref(d)) == 0, bad
+        assert L.ic_sparse_attn_kv4(C.byref(d), None, 200, ONE, ONE, ONE, ONE, None, ONE, 1 << 40, None) in (S.ERR_UNSUPPORTED, S.ERR_SHAPE)
