@@ -303,7 +303,7 @@ ic_status ic_attn_probs_kv4(const ic_attn_desc *desc, const ic_paged_cache *pc, 
  * ic_evict_keep: the positions of each sequence that stay when at most n_keep do.  A sequence of n = min(Lk, seq_lens[b])
  *   positions (seq_lens NULL: Lk) keeps all if n <= n_keep; otherwise the first n_first, the last n_recent, and of the
  *   others those with the largest weight[b,s] up to n_keep in all (equal weights: the lower position; NaN counts as the
- *   largest).  n_first + n_recent <= n_keep <= Lk.
+ *   largest).  n_first + n_recent <= n_keep <= Lk <= 2^31 - 8192.
  *   keep [B,n_keep] int32 out: the positions in ASCENDING order, then -1;  keep_lens [B] int32 out: their number, the new
  *   seq_lens;  keep_weight [B,n_keep] fp32 out, nullable: weight at those positions (0 behind them), the new weight.
  *   None of the three may overlap another, weight or seq_lens (IC_ERR_SHAPE): the new lengths and weights are buffers of their own.

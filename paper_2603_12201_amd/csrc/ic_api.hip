@@ -1814,7 +1814,7 @@ ic_status ic_attn_weight_add(int32_t B, int32_t Tq, int32_t k_sel, int32_t Lk, c
 
 size_t ic_evict_keep_workspace(int32_t B, int32_t Lk)
 {
-    if (B <= 0 || Lk <= 0 || (int64_t)B * Lk > INT32_MAX) return 0;
+    if (B <= 0 || Lk <= 0 || Lk > ic::kEvictMaxLk || (int64_t)B * Lk > INT32_MAX) return 0;
     return align_up(ic::evict_ws_bytes(B, Lk));
 }
 
@@ -1827,6 +1827,7 @@ ic_status ic_evict_keep(int32_t B, int32_t Lk, const float *weight, const int32_
     if (n_keep > Lk || (int64_t)n_first + n_recent > n_keep)
         return fail(IC_ERR_SHAPE, "need n_first + n_recent <= n_keep <= Lk (%d + %d, %d, %d)", n_first, n_recent, n_keep, Lk);
     if ((int64_t)B * Lk > INT32_MAX) return fail(IC_ERR_SHAPE, "B*Lk too large");
+    if (Lk > ic::kEvictMaxLk) return fail(IC_ERR_UNSUPPORTED, "Lk=%d exceeds %d", Lk, ic::kEvictMaxLk);
     if (!weight || !keep || !keep_lens) return fail(IC_ERR_NULL, "weight, keep and keep_lens must not be NULL");
     ic_status s = check_ws(workspace, workspace_bytes, ic_evict_keep_workspace(B, Lk));
     if (s != IC_OK) return s;

@@ -240,6 +240,9 @@ struct WeightArgs {
     int32_t range, n_ranges, chunk_rows, n_chunks;
 };
 
+constexpr int kEvictPart = 8192;                           // positions of a part of a long sequence
+constexpr int kEvictMaxLk = INT32_MAX - (kEvictPart - 1);  // every part ends in 32 bits
+
 // Which positions stay.
 struct EvictArgs {
     const float *weight;  // [B,Lk]

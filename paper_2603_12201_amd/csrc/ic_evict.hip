@@ -288,7 +288,7 @@ __global__ __launch_bounds__(kEvictThreads) void evict_kernel(EvictArgs a)
 // workgroups' histograms of the digit before it (4 KB each) by itself.  Bound by latency: weights, histograms, LDS additions one
 // after the other.  200 000 positions: 28 us in four launches (430 in one workgroup; 35 with 16384 positions and 8 KB each, 29
 // with 4096), 32 sequences of 65536 in 30.
-constexpr int kPartR = 8, kPart = kPartR * kEvictThreads;
+constexpr int kPart = kEvictPart, kPartR = kPart / kEvictThreads;
 struct PartCounts {
     unsigned int hist[2][1024], last[512];    // two bins a word: a part has no more than 8192 keys
     unsigned int above[2];                    // inner keys above the border by the first digit; by the second

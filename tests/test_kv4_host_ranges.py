@@ -1,7 +1,5 @@
 """What the eviction entry points refuse about where their buffers lie and how long their sequences are, before anything is launched;
 no GPU needed (addresses that nothing reads)."""
-import ctypes as C
-
 import pytest
 
 FAR = 1 << 30
@@ -14,8 +12,8 @@ def ic():
     return m
 
 
-def _evict(ic, B=2, Lk=1000, n_keep=400, weight=FAR, lens=2 * FAR, keep=3 * FAR, keep_lens=4 * FAR, kept=5 * FAR):
-    return ic.lib().ic_evict_keep(B, Lk, weight, lens, n_keep, 4, 16, keep, keep_lens, kept, 6 * FAR, 1 << 40, None)
+def _evict(ic, B=2, Lk=1000, n_keep=400, weight=FAR, lens=2 * FAR, keep=3 * FAR, keep_lens=4 * FAR, kept=5 * FAR, have=1 << 40):
+    return ic.lib().ic_evict_keep(B, Lk, weight, lens, n_keep, 4, 16, keep, keep_lens, kept, 6 * FAR, have, None)
 
 
 def test_what_stays_is_not_written_over_what_is_read(ic):
@@ -42,3 +40,13 @@ def test_weights_are_not_written_over_what_is_read(ic):
     S = ic.Status
     assert add(w=FAR) == S.ERR_SHAPE and add(w=FAR + 4 * (2 * 3 * 64 - 1)) == S.ERR_SHAPE and add(w=2 * FAR - 4 * (2 * 1000 - 1)) == S.ERR_SHAPE
     assert add(w=3 * FAR + 4) == S.ERR_SHAPE and add(w=3 * FAR - 4 * 1000) == S.ERR_SHAPE   # (the same address is in place, and allowed)
+
+
+def test_sequences_whose_last_part_would_pass_32_bits(ic):
+    """Parts of 8192 positions are numbered in 32 bits."""
+    L, S = ic.lib(), ic.Status
+    most = (1 << 31) - 8192
+    assert L.ic_evict_keep_workspace(1, most) > 0 and _evict(ic, B=1, Lk=most, weight=1 << 40, have=0) == S.ERR_WORKSPACE
+    for Lk in (most + 1, (1 << 31) - 1):
+        assert L.ic_evict_keep_workspace(1, Lk) == 0
+        assert _evict(ic, B=1, Lk=Lk, weight=1 << 40) == S.ERR_UNSUPPORTED
