@@ -61,8 +61,8 @@ __global__ __launch_bounds__(kWeightThreads) void weight_kernel(WeightArgs a)
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u) {
             const int e = u * kWeightThreads + tid;
-            s[u] = ie[min(e, left - 1)] - lo;
-            s[u] = e < left && s[u] >= 0 && s[u] < n ? s[u] : -1;
+            const unsigned int at = (unsigned)ie[min(e, left - 1)] - (unsigned)lo;   // (of a negative entry: 2^31 - lo or more, behind n)
+            s[u] = e < left && at < (unsigned)n ? (int)at : -1;
         }
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u) v[u] = pe[s[u] >= 0 ? u * kWeightThreads + tid : 0];
@@ -436,6 +436,9 @@ __global__ __launch_bounds__(256) void compact_kernel(CompactArgs a)
 
 } // namespace
 
+// n things by `per` (both may be near 2^31).
+static int groups(int n, int per) { return (n - 1) / per + 1; }
+
 // Ranges and chunks of a call.  One chunk: the launch writes the weights itself.
 // A range is what LDS holds, as every range's workgroup goes through all of the entries; with no more than 16 of them per
 // position of a short range that costs less than the positions, and four times the workgroups take them (32 sequences of 65536
@@ -444,16 +447,16 @@ void weight_plan(WeightArgs &a)
 {
     const int most = (int64_t)a.Tq * a.k_sel <= 16 * kFewRange ? kFewRange : kMaxRange;
     a.range = a.Lk < most ? a.Lk : most;
-    a.n_ranges = (a.Lk + a.range - 1) / a.range;
+    a.n_ranges = groups(a.Lk, a.range);
     int chunks = 1;
     if (a.Tq > 16) {
         chunks = 256 / (a.B * a.n_ranges > 256 ? 256 : a.B * a.n_ranges);
         if (chunks > a.Tq / 16) chunks = a.Tq / 16;
     }
-    const int least = (a.Tq + kMaxChunkRows - 1) / kMaxChunkRows;
+    const int least = groups(a.Tq, kMaxChunkRows);
     if (chunks < least) chunks = least;
-    a.chunk_rows = (a.Tq + chunks - 1) / chunks;
-    a.n_chunks = (a.Tq + a.chunk_rows - 1) / a.chunk_rows;
+    a.chunk_rows = groups(a.Tq, chunks);
+    a.n_chunks = groups(a.Tq, a.chunk_rows);
 }
 
 hipError_t launch_weight_add(const WeightArgs &a, hipStream_t st)

@@ -230,3 +230,18 @@ def test_together_as_a_server_uses_them(ic):
     assert new_lens.cpu().tolist() == [n_keep, n_keep, 134]
     assert torch.equal(O, O2) and torch.equal(lse, lse2)                         # the same rows in the same order
     assert torch.equal(kept, torch.where(keep >= 0, weight.gather(1, keep.clamp(min=0).long()), torch.zeros_like(kept)))
+
+
+def test_weights_of_the_most_positions(ic):
+    """2^31 - 1 positions (8.6 GB), of which a few receive something."""
+    say("weights of 2^31 - 1 positions")
+    Lk = (1 << 31) - 1
+    at = [0, 1, 4095, 4096, 16383, 16384, 1 << 30, Lk - 16384, Lk - 2, Lk - 1]
+    idx = torch.tensor([[at + [-1, -(1 << 31)]]], dtype=torch.int32, device="cuda")
+    p = torch.arange(1, len(at) + 3, device="cuda").float().reshape(1, 1, -1) / 64
+    w = torch.zeros((1, Lk), device="cuda")
+    ic.attn_weight_add(p, idx, w)
+    got = w[0, torch.tensor(at, device="cuda")]
+    assert torch.equal(got, p[0, 0, :len(at)])
+    w[0, torch.tensor(at, device="cuda")] = 0
+    assert not any(bool(c.any()) for c in w[0].split(1 << 28))

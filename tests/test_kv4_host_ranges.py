@@ -50,3 +50,9 @@ def test_sequences_whose_last_part_would_pass_32_bits(ic):
     for Lk in (most + 1, (1 << 31) - 1):
         assert L.ic_evict_keep_workspace(1, Lk) == 0
         assert _evict(ic, B=1, Lk=Lk, weight=1 << 40) == S.ERR_UNSUPPORTED
+
+
+def test_chunks_of_the_most_query_rows(ic):
+    """No chunk has more than 2^15 rows, whose sums fit 64 bits: 65536 chunks of 100 positions, 8 bytes each."""
+    assert ic.lib().ic_attn_weight_add_workspace(1, (1 << 31) - 1, 1, 100) == 65536 * 100 * 8
+    assert ic.lib().ic_attn_weight_add_workspace(1, 1 << 30, 1, 100) == 32768 * 100 * 8
