@@ -417,8 +417,9 @@ __global__ __launch_bounds__(256) void compact_kernel(CompactArgs a)
 {
     __shared__ int64_t src[kMoveRows], dst[kMoveRows];
     const int tid = threadIdx.x, c = blockIdx.y;
-    const int per_seq = (a.n_keep + kMoveRows - 1) / kMoveRows;
-    const int b = blockIdx.x / per_seq, j0 = (blockIdx.x - b * per_seq) * kMoveRows;
+    const unsigned int per_seq = (unsigned)(a.n_keep - 1) / kMoveRows + 1, at = blockIdx.z * gridDim.x + blockIdx.x;   // (see launch_compact())
+    if (at / per_seq >= (unsigned)a.B) return;
+    const int b = (int)(at / per_seq), j0 = (int)(at - b * per_seq) * kMoveRows;
     if (tid < kMoveRows) {
         const int j = j0 + tid;
         const int s = j < a.n_keep ? a.keep[(int64_t)b * a.n_keep + j] : -1;
@@ -513,8 +514,9 @@ hipError_t launch_evict_keep(EvictArgs a, hipStream_t st)
 
 hipError_t launch_compact(const CompactArgs &a, hipStream_t st)
 {
-    const int per_seq = (a.n_keep + kMoveRows - 1) / kMoveRows;
-    const dim3 grid((unsigned)(a.B * per_seq), (unsigned)a.n_caches), block(256);
+    // a dimension of a launch has less than 2^32 threads: 2^23 workgroups a step of z, up to 2^31 of them
+    const int64_t wgs = (int64_t)a.B * groups(a.n_keep, kMoveRows), x = wgs < (1 << 23) ? wgs : 1 << 23;
+    const dim3 grid((unsigned)x, (unsigned)a.n_caches, (unsigned)((wgs + x - 1) / x)), block(256);
     int64_t bytes = 0;
     for (int c = 0; c < a.n_caches; ++c) bytes += (int64_t)a.B * a.n_keep * a.row_bytes[c];
     // What is more than the last cache holds (256 MB) goes past the caches: the step behind would not find it there, and it is faster

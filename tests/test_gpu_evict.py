@@ -245,3 +245,16 @@ def test_weights_of_the_most_positions(ic):
     assert torch.equal(got, p[0, 0, :len(at)])
     w[0, torch.tensor(at, device="cuda")] = 0
     assert not any(bool(c.any()) for c in w[0].split(1 << 28))
+
+
+def test_more_rows_than_one_dimension_of_a_launch(ic):
+    """2^29 + 5 rows of 4 bytes: more workgroups of 256 threads than 2^32 threads have."""
+    n = (1 << 29) + 5
+    say("compact %d rows" % n)
+    src = torch.arange(n + 3, dtype=torch.int32, device="cuda").view(1, -1, 1)
+    keep = torch.arange(3, n + 3, dtype=torch.int32, device="cuda").view(1, -1)
+    keep[0, 7] = -1
+    dst = torch.full((1, n, 1), -9, dtype=torch.int32, device="cuda")
+    ic.cache_compact([(src, dst)], keep, n + 3)
+    keep[0, 7] = -9
+    assert torch.equal(dst.view(1, -1), keep)
