@@ -1,10 +1,11 @@
 """A selected row of the 4-bit cache that holds no numbers, whether its query is split over workgroups or not: the query's output,
 log-sum-exp and probabilities are none either, its weights stay what they were, and no other query sees anything of it."""
+import numpy as np
 import pytest
 import torch
 
 from tests import kv4_ref
-from tests.test_gpu_kv4 import SCALE, Paged, bits, rows_of
+from tests.test_gpu_kv4 import SCALE, Paged, bits, check_query, rows_of
 
 pytestmark = pytest.mark.gpu
 
@@ -58,3 +59,37 @@ def test_a_row_without_numbers_spoils_its_query_only(ic, B, k, kind, page):
     O, lse, p, w = got[1]
     assert O[bad].isnan().all() and lse[bad].isnan().all() and p[bad].isnan().all()
     assert torch.equal(w[bad], w0[bad])
+
+
+# few queries, a wave each with the weights four waves to a query, and a wave each for both
+@pytest.mark.parametrize("T", [2, 600, 800])
+@pytest.mark.parametrize("paged", [False, True])
+def test_rows_on_both_sides_of_4_gib(ic, T, paged):
+    """11.2 million rows: some in front of the first that begins behind 4 GiB, some around it, some at the end."""
+    n = 175000 * 64
+    first = -(-(1 << 32) // 400)
+    print(f"[case] {T} queries over {n} rows, paged {paged}", flush=True)
+    kv4 = torch.empty((n, 400), dtype=torch.uint8, device="cuda")
+    x = rows_of(14, 192, wide=False)
+    at = [0, first - first % 64, n - 64]
+    if paged:
+        Lk, pc = 192, ic.paged_cache(None, torch.tensor([[a // 64 for a in at]], dtype=torch.int32, device="cuda"), 64)
+        pos = np.arange(192)
+        ic.kv4_write(x.cuda()[None], kv4, Lk=Lk, pc=pc)
+    else:
+        Lk, pc = n, None
+        kv4 = kv4[None]
+        pos = np.concatenate([np.arange(a, a + 64) for a in at])
+        for i, a in enumerate(at):
+            ic.kv4_write(x[64 * i:64 * i + 64].cuda()[None], kv4, pos0=a)
+    want = kv4_ref.pack(bits(x))
+    for i, a in enumerate(at):
+        assert np.array_equal(kv4.view(n, 400)[a:a + 64].cpu().numpy(), want[64 * i:64 * i + 64])
+    Q = torch.randn((1, T, 32, 576), generator=torch.Generator().manual_seed(3)).to(torch.bfloat16)
+    sel = np.stack([np.sort(np.random.default_rng(t).permutation(192)[:150]) for t in range(T)])
+    idx = torch.from_numpy(pos[sel].astype(np.int32)).cuda()[None]
+    O, lse = ic.sparse_attn_kv4(Q.cuda(), kv4, idx, SCALE, Lk=Lk, pc=pc, want_lse=True)
+    probs = ic.attn_probs_kv4(Q.cuda(), kv4, idx, SCALE, lse, Lk=Lk, pc=pc)
+    rows, Qf = kv4_ref.unpack(want), kv4_ref.bf16_bits_to_f64(bits(Q))
+    for t in sorted({0, 1, T // 2, T - 1}):
+        check_query(O[0, t], lse[0, t], probs[0, t], Qf[0, t], rows[sel[t]], np.ones(150, dtype=bool))
