@@ -420,6 +420,23 @@ __device__ __forceinline__ float half_sum(float x)
     return as_float(y[0]) + as_float(y[1]);
 }
 
+// The exponents of P are s scale - ref, in one rounding, with the reference's own bias in ref = m - kPBias.  By references of
+// kFar and more those roundings are powers of two of their own (at 2^30, 64 of them) and P would leave the range of a float: there
+// the scores are by the reference before they are scaled, s' = (s scale - m) / scale, rounded as m is, and ref is the bias alone.
+constexpr float kFar = 0x1p20f;
+__device__ __forceinline__ float far_scores(f32x16 &s, float m, float ref, float scale)
+{
+#pragma clang fp contract(off)
+    if (__ballot(__builtin_fabsf(m) >= kFar && m != -INFINITY) == 0ull) return ref;
+    const float by = m == -INFINITY ? 0.f : m, back = __builtin_amdgcn_rcpf(scale);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const float z = s[i] * scale;
+        s[i] = (z - by) * back;
+    }
+    return m == -INFINITY ? 0.f : -kPBias;
+}
+
 // O^T times a factor per head, a tile at a time: the accumulators live in registers that only matrix instructions and moves
 // reach, and all of them out at once would displace everything else.
 template <int N> __device__ __forceinline__ void scale_tiles(f32x16 (&o)[N], float f)
@@ -691,7 +708,7 @@ __global__ __launch_bounds__(256, 1) void kv4_attn_kernel(Kv4AttnArgs a)
                 keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
                 m = mn;
                 l *= keep;
-                ref = m == -INFINITY ? 0.f : m - kPBias;
+                ref = far_scores(s, m, m == -INFINITY ? 0.f : m - kPBias, a.scale_log2e);
             }
             if (i >= 12 && i < 28) {
                 const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i - 12], a.scale_log2e, -ref));
@@ -903,7 +920,7 @@ __global__ __launch_bounds__(256, 1) void kv4_attn_few_kernel(Kv4AttnArgs a)
             l *= keep;
             scale_tiles(o, keep);
         }
-        const float ref = m == -INFINITY ? 0.f : m - kPBias;
+        const float ref = far_scores(s, m, m == -INFINITY ? 0.f : m - kPBias, a.scale_log2e);
         u32x4 p[2];
 #pragma unroll
         for (int i = 0; i < 16; i += 2) {

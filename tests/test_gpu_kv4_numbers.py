@@ -93,3 +93,51 @@ def test_rows_on_both_sides_of_4_gib(ic, T, paged):
     rows, Qf = kv4_ref.unpack(want), kv4_ref.bf16_bits_to_f64(bits(Q))
     for t in sorted({0, 1, T // 2, T - 1}):
         check_query(O[0, t], lse[0, t], probs[0, t], Qf[0, t], rows[sel[t]], np.ones(150, dtype=bool))
+
+
+@pytest.mark.parametrize("T, k", [(1, 40), (1, 700), (40, 2048), (300, 300), (700, 200)])
+@pytest.mark.parametrize("power", [20, 25, 26, 27, 28, 29, 30, 31, 40, 90])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_scores_of_any_size(ic, T, k, power, sign):
+    """One feature decides: row r scores sign (1 + r / 64 % 1) 2^power, exactly, so that equal rows share the weight and it is their mean."""
+    print(f"[case] {T} queries of {k} rows, scores about {sign} 2^{power}", flush=True)
+    x = rows_of(17, k, wide=False)
+    x[:, 512:] = 0
+    step = torch.arange(k) * 7 % 64
+    x[:, 512] = sign * (1 + step / 64.0) * 2.0 ** (power // 2)
+    Q = torch.zeros((1, T, 32, 576), dtype=torch.bfloat16)
+    Q[..., 512] = 2.0 ** (power - power // 2)
+    kv4 = torch.empty((1, k, 400), dtype=torch.uint8, device="cuda")
+    ic.kv4_write(x.cuda()[None], kv4)
+    idx = torch.arange(k, dtype=torch.int32, device="cuda").expand(1, T, k).contiguous()
+    O, lse = ic.sparse_attn_kv4(Q.cuda(), kv4, idx, 1.0, want_lse=True)
+    top = int(step.max() if sign > 0 else step.min())
+    rows = kv4_ref.unpack(kv4.cpu().numpy()[0])[(step == top).numpy()]
+    want = rows[:, :512].mean(0)
+    # weights 1 / n in bf16, 2^-8 each, and the output's 2^-8; the next lower scores are 2^(power - 6) further down
+    tol = 2.0 ** -8 * np.abs(rows[:, :512]).mean(0) + 2.0 ** -8 * np.abs(want) + 2.0 ** -20
+    assert np.all(np.abs(O[0].double().cpu().numpy() - want) <= tol)
+    l = sign * (1 + top / 64.0) * 2.0 ** power + np.log(len(rows))
+    assert np.all(np.abs(lse.double().cpu().numpy() - l) <= 2.0 ** -20 * (1 + abs(l)))
+
+
+@pytest.mark.parametrize("B, k", [(2, 2048), (40, 2048), (300, 300), (600, 200)])
+def test_a_score_of_minus_infinity_is_a_skipped_entry(ic, B, k):
+    print(f"[case] {B} queries of {k} rows, -inf", flush=True)
+    packed = kv4_ref.pack(bits(rows_of(B, k, wide=False)))
+    gone = [0, 5, k // 2, k - 1] + list(range(64, 128))                          # (whole tiles among them)
+    packed[gone, 256:258] = (0x80, 0xFF)
+    kv4 = torch.from_numpy(packed).cuda()[None].expand(B, k, 400).contiguous()
+    Q = torch.randn((B, 1, 32, 576), generator=torch.Generator().manual_seed(k)).to(torch.bfloat16)
+    Q[..., 512] = Q[..., 512].abs().clamp_min(0.1)
+    idx = torch.arange(k, dtype=torch.int32, device="cuda").expand(B, 1, k).contiguous()
+    skip = idx.clone()
+    skip[..., gone] = -1
+    got, want = [ic.sparse_attn_kv4(Q.cuda(), kv4, i, SCALE, want_lse=True) for i in (idx, skip)]
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    p, q = [ic.attn_probs_kv4(Q.cuda(), kv4, i, SCALE, want[1]) for i in (idx, skip)]
+    assert torch.equal(p, q)
+    only = torch.full_like(idx, -1)                                              # nothing but such rows
+    only[..., gone] = idx[..., gone]
+    O, lse = ic.sparse_attn_kv4(Q.cuda(), kv4, only, SCALE, want_lse=True)
+    assert not O.any() and bool((lse == -float("inf")).all())
