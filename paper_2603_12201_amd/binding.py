@@ -593,6 +593,13 @@ def _same_device(*tensors):
             raise IcError(Status.ERR_SHAPE, "a tensor %s is on %s, the current device is %d" % (tuple(t.shape), t.device, here))
 
 
+def _stream_here(stream):
+    """The stream's handle; it has to be of the current device, like the tensors."""
+    if stream is not None and getattr(stream, "device_index", None) not in (None, _current_device()):
+        raise IcError(Status.ERR_SHAPE, "the stream is of device %d, the current device is %d" % (stream.device_index, _current_device()))
+    return _stream(stream)
+
+
 def _kv4_cache(kv4, B, Lk, pc):
     """Checks a 4-bit cache against its layout; returns (Lk, rows that it holds)."""
     import torch
@@ -631,7 +638,7 @@ def kv4_write(rows, kv4, pos0=0, Lk=None, pc=None, stream=None):
     Lk, n = _kv4_cache(kv4, B, Lk, pc)
     _same_device(kv4, rows)
     d = Kv4Desc(B, Tn, Lk, 0, pos0, n)
-    _check(lib().ic_kv4_write(C.byref(d), _ref(pc), _ptr(rows), _ptr(kv4), _stream(stream)))
+    _check(lib().ic_kv4_write(C.byref(d), _ref(pc), _ptr(rows), _ptr(kv4), _stream_here(stream)))
     return kv4
 
 
@@ -647,7 +654,7 @@ def kv4_read(kv4, B, Tn, pos0=0, Lk=None, pc=None, stream=None, out=None):
         raise IcError(Status.ERR_SHAPE, "out %s must be %s" % (tuple(out.shape), (B, Tn, 576)))
     _same_device(kv4, out)
     d = Kv4Desc(B, Tn, Lk, 0, pos0, n)
-    _check(lib().ic_kv4_read(C.byref(d), _ref(pc), _ptr(kv4), _ptr(out), _stream(stream)))
+    _check(lib().ic_kv4_read(C.byref(d), _ref(pc), _ptr(kv4), _ptr(out), _stream_here(stream)))
     return out
 
 
@@ -678,7 +685,7 @@ def sparse_attn_kv4(Q, kv4, idx, sm_scale, Lk=None, pc=None, want_lse=False, wor
             raise IcError(Status.ERR_SHAPE, "out %s must be %s" % (tuple(O.shape), (d.B, d.Tq, d.H_q, 512)))
     _same_device(kv4, Q, idx, O, workspace)
     _check(lib().ic_sparse_attn_kv4(C.byref(d), _ref(pc), n, _ptr(Q), _ptr(kv4), _ptr(idx), _ptr(O), _ptr(lse), _ptr(workspace),
-                                    _bytes_of(workspace), _stream(stream)))
+                                    _bytes_of(workspace), _stream_here(stream)))
     return (O, lse) if want_lse else O
 
 
@@ -693,7 +700,7 @@ def attn_probs_kv4(Q, kv4, idx, sm_scale, lse, Lk=None, pc=None, stream=None):
     _same_device(kv4, Q, idx, lse)
     with _on(stream):
         probs = lse.new_empty(idx.shape)
-    _check(lib().ic_attn_probs_kv4(C.byref(d), _ref(pc), n, _ptr(Q), _ptr(kv4), _ptr(idx), _ptr(lse), _ptr(probs), _stream(stream)))
+    _check(lib().ic_attn_probs_kv4(C.byref(d), _ref(pc), n, _ptr(Q), _ptr(kv4), _ptr(idx), _ptr(lse), _ptr(probs), _stream_here(stream)))
     return probs
 
 
@@ -717,7 +724,7 @@ def attn_weight_add(probs, idx, weight, out=None, workspace=None, stream=None):
             with _on(stream):
                 workspace = _workspace(need, weight)
     _check(lib().ic_attn_weight_add(B, Tq, k, Lk, _ptr(probs), _ptr(idx), _ptr(weight), _ptr(out), _ptr(workspace),
-                                    _bytes_of(workspace), _stream(stream)))
+                                    _bytes_of(workspace), _stream_here(stream)))
     return out
 
 
@@ -742,7 +749,7 @@ def evict_keep(weight, n_keep, n_first=0, n_recent=0, seq_lens=None, workspace=N
         lens = weight.new_empty((B,), dtype=torch.int32)
         kept = weight.new_empty((B, n_keep))
     _check(lib().ic_evict_keep(B, Lk, _ptr(weight), _ptr(seq_lens), n_keep, n_first, n_recent, _ptr(keep), _ptr(lens), _ptr(kept),
-                               _ptr(workspace), _bytes_of(workspace), _stream(stream)))
+                               _ptr(workspace), _bytes_of(workspace), _stream_here(stream)))
     return keep, lens, kept
 
 
@@ -771,7 +778,7 @@ def cache_compact(caches, keep, Lk, src_pc=None, dst_pc=None, stream=None):
             raise IcError(Status.ERR_SHAPE, "src %s and dst %s must be [%d, %d, ..] and [%d, %d, ..]" % (tuple(ss), tuple(ds), B, Lk, B, n_keep))
         m.src, m.dst, m.src_rows, m.dst_rows = src.data_ptr(), dst.data_ptr(), ss[:rs].numel(), ds[:rd].numel()
         m.row_bytes, m.reserved = src.element_size() * ss[rs:].numel(), 0
-    _check(lib().ic_cache_compact(moves, len(caches), B, Lk, n_keep, _ptr(keep), _ref(src_pc), _ref(dst_pc), _stream(stream)))
+    _check(lib().ic_cache_compact(moves, len(caches), B, Lk, n_keep, _ptr(keep), _ref(src_pc), _ref(dst_pc), _stream_here(stream)))
 
 
 def debug_indexer_scores(q, k, w, q_pos0, row0, n_rows, q_scale=None, k_scale=None, stream=None):
