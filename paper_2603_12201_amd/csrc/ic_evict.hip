@@ -61,8 +61,8 @@ __global__ __launch_bounds__(kWeightThreads) void weight_kernel(WeightArgs a)
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u) {
             const int e = u * kWeightThreads + tid;
-            const unsigned int at = (unsigned)ie[min(e, left - 1)] - (unsigned)lo;   // (of a negative entry: 2^31 - lo or more, behind n)
-            s[u] = e < left && at < (unsigned)n ? (int)at : -1;
+            s[u] = (int)((unsigned)ie[min(e, left - 1)] - (unsigned)lo);    // (without overflow for any entry)
+            s[u] = e < left && s[u] >= 0 && s[u] < n ? s[u] : -1;
         }
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u) v[u] = pe[s[u] >= 0 ? u * kWeightThreads + tid : 0];
