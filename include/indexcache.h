@@ -267,9 +267,10 @@ ic_status ic_distill_loss(const float *const *probs, int32_t n_targets, const fl
  *
  * ic_sparse_attn_kv4: ic_sparse_attn over such a cache: the same as over the rows that ic_kv4_read returns, with
  *   desc->d_qk = row_elems = 576, d_v = 512, v_off = 0.  With seq_lens, entries of idx at or behind seq_lens[b] are skipped too.
- *   A skipped entry's row never matters, whatever it holds.
+ *   A skipped entry's row never matters, whatever it holds.  A score of -inf counts for nothing; a row with one that is not a
+ *   number, or +inf, has a NaN output and log-sum-exp, and no other row sees anything of it.
  * ic_attn_probs_kv4: ic_attn_probs over such a cache; lse as ic_sparse_attn_kv4 returns it.  Rows without a valid entry give
- *   zeros (their lse is not used).
+ *   zeros (their lse is not used), rows whose lse is NaN give NaN, which ic_attn_weight_add counts as 0.
  * Q, rows and O: addresses that are multiples of 16.  Asynchronous; errors as elsewhere, IC_ERR_SHAPE for a bad address.
  */
 #define IC_KV4_ROW_BYTES 400
@@ -495,8 +496,9 @@ ic_status ic_calibrate(int32_t kind, const void *src, void *dst, const int32_t *
 
 /*
  * Per-kernel timing with HIP events recorded on the launch stream (a measuring aid; off by
- * default).  ic_prof_enable(1) starts recording an event pair around every kernel launch
- * (bounded pool of 8192 pairs; launches beyond it are not recorded), ic_prof_enable(0) stops.
+ * default).  ic_prof_enable(1) starts recording an event pair around every kernel launch of the
+ * classes below (of the indexer, of the sparse attentions and of their merges; no others are
+ * recorded, nor those beyond a bounded pool of 8192 pairs), ic_prof_enable(0) stops.
  * ic_prof_collect waits for the recorded events (host-blocking) and adds their durations to
  * per-class totals; ic_prof_get reads the totals of kernel class `which`
  * (0 = indexer score, 1 = top-k select, 2 = sparse attention, 3 = attention split merge):

@@ -12,8 +12,8 @@
 // for N(0,1) features the relative error is 0.125, and 0.115 with blocks of 32.
 //
 //   kv4_write_kernel  one wave per row: 16 lanes a block, its maximum by data-parallel moves, codes by the converting
-//                     instruction (ties to the even code).  Bound by memory: 1152 bytes in, 400 out; 131072 rows 41 us,
-//                     4.9 TB/s, what a large copy reaches.
+//                     instruction (ties to the even code).  Bound by memory: 1152 bytes in, 400 out; 131072 rows 41 to
+//                     45 us, 4.5 to 4.9 TB/s, what a large copy reaches.
 //   kv4_read_kernel   the way back to bf16, exact: the same rows in 31 us behind the former.
 //   kv4_attn_kernel, kv4_attn_few_kernel
 //                     O = softmax(sm_scale Q K^T) V over the rows that idx names.  See there.
@@ -160,7 +160,7 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4RowsArgs a)
 //       times 2^100 (kMaxE) so that the difference is never negative.
 // The rows' bytes go from memory into LDS without passing through registers; the codes of four tiles, 8 KB each, and the
 // rotary part of one are what a wave has there: bf16 tiles would be three times as large.  No wave waits for another.
-// 32768 queries of 2048 rows: 4.8 ms, 950 TFLOP/s where a plain product of 8192^3 reaches 1141.  Bound by issue: an instruction
+// 32768 queries of 2048 rows: 4.7 ms, 965 TFLOP/s where a plain product of 8192^3 reaches 1141.  Bound by issue: an instruction
 // takes a wave 4.3 to 4.7 clocks, a product 13, and a tile has some 850, 68 of them products (without the fetches 4.2 ms; the fetches alone 2.4).
 // Registers: 256 of O^T, 144 of Q and about 100 more: one wave per SIMD, which issues in order, so the 68 matrix instructions
 // of a tile (32 clocks each) have the rest, about 6 vector instructions each, dealt out between them by hand: a step multiplies
@@ -1009,8 +1009,8 @@ __global__ __launch_bounds__(256, 1) void kv4_attn_few_kernel(Kv4AttnArgs a)
 // probs[q, slot] = 1/H sum_h exp(sm_scale <Q[h], K[row]> - lse[h]).  The same tiles as above with the operands exchanged:
 // heads are the matrix rows, cache rows the columns, so a lane holds 16 heads of one cache row and adds them up by itself.
 // A step multiplies one tile and, between its products, takes the exponentials of the tile before.  What bounds it are the
-// rows' lines from L2: 8191 queries of 2048 rows in 690 us, 9.7 TB/s of rows, where the fetches of kv4_attn_kernel without its
-// arithmetic ran at 11.4 (a row of 400 bytes lies in 5 lines of 128, asked for as 6).
+// rows' lines from L2: 8191 queries of 2048 rows in 600 us, 11.2 TB/s of rows, what the fetches of kv4_attn_kernel without its
+// arithmetic ran at (a row of 400 bytes lies in 5 lines of 128, asked for as 6).
 struct ProbTiles {
     static constexpr int kSlotB = kCodeB;
     unsigned char code[4][3][kCodeB];         // [wave][ring]
@@ -1207,7 +1207,7 @@ hipError_t launch_kv4_read(const Kv4RowsArgs &a, hipStream_t st)
     return hipGetLastError();
 }
 
-// Whether every row of the cache begins below 4 GB (with the bytes behind a row's beginning that are added to it).
+// Whether a row of the cache begins behind 4 GB, where an offset of 32 bits does not reach (the bytes within a row that are added to it included).
 bool kv4_wide(const Kv4AttnArgs &a) { return (uint64_t)a.pool_rows * kRowB > 0xFFFFFFFFull; }
 
 // Kernel forms by what a cache is.
