@@ -308,7 +308,7 @@ __global__ __launch_bounds__(kEvictThreads) void evict_part_kernel(EvictArgs a)
     const int lo = a.n_first, hi = len - a.n_recent, want = a.n_keep - a.n_first - a.n_recent;
     const int p0 = part * kPart;
     if (p0 >= len || (LEVEL < 3 && want == 0)) return;
-    const int live = (len + kPart - 1) / kPart;                             // parts that hold positions
+    const int live = (len - 1) / kPart + 1;                                 // parts that hold positions
     PartCounts *const seq = (PartCounts *)a.ws + (int64_t)b * a.n_parts, *const own = seq + part;
     float w[kPartR];
     unsigned int key[kPartR];
@@ -483,7 +483,7 @@ hipError_t launch_weight_add(const WeightArgs &a, hipStream_t st)
 // 49 and 33; 16384: 19 and 16, 20 and 17, 33 and 20).
 int evict_parts(int B, int Lk)
 {
-    const int parts = (Lk + kPart - 1) / kPart;
+    const int parts = groups(Lk, kPart);
     return Lk > 32 * kEvictThreads || (Lk > 16 * kEvictThreads && (int64_t)B * parts <= 256) ? parts : 0;
 }
 size_t evict_ws_bytes(int B, int Lk) { return (size_t)B * evict_parts(B, Lk) * sizeof(PartCounts); }
