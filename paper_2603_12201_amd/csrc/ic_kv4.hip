@@ -160,7 +160,7 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4RowsArgs a)
 //       times 2^100 (kMaxE) so that the difference is never negative.
 // The rows' bytes go from memory into LDS without passing through registers; the codes of four tiles, 8 KB each, and the
 // rotary part of one are what a wave has there: bf16 tiles would be three times as large.  No wave waits for another.
-// 32768 queries of 2048 rows: 4.7 ms, 965 TFLOP/s where a plain product of 8192^3 reaches 1141.  Bound by issue: an instruction
+// 32768 queries of 2048 rows: 4.7 to 4.8 ms, 940 to 965 TFLOP/s where a plain product of 8192^3 reaches 1141.  Bound by issue: an instruction
 // takes a wave 4.3 to 4.7 clocks, a product 13, and a tile has some 850, 68 of them products (without the fetches 4.2 ms; the fetches alone 2.4).
 // Registers: 256 of O^T, 144 of Q and about 100 more: one wave per SIMD, which issues in order, so the 68 matrix instructions
 // of a tile (32 clocks each) have the rest, about 6 vector instructions each, dealt out between them by hand: a step multiplies
